@@ -442,6 +442,106 @@ int bnn_semi_stochastic_binarize(float* w, const float* u, int64_t count, void* 
  *   subtraction.  The two buffers must not overlap (BNN_EINVAL).  M = 0 is a no-op. */
 int bnn_subtract_log_prior(float* logp, const float* log_prior, int64_t M, int64_t N, void* stream);
 
+/* ------------------------------------------------------------------------------------------------------------------
+ * 4-bit layers: weights and inputs in microscaled 4-bit floating point, for layers that do not bear one bit (the paper keeps
+ * the input and the Softmax layer in real numbers, Sec. 2.2 and 3.1): 4.25 bits per number, products on the 4-bit matrix cores.
+ *
+ * Format (the OCP microscaling format MXFP4).  The K numbers of a row go in blocks of 32; a number is 2^(e - 127) times one of
+ * 0, 0.5, 1, 1.5, 2, 3, 4, 6 (codes 0 to 7, bit 3 the sign), e being the block's scale byte.  e = 255 makes the block NaN.
+ * A matrix [R][K] is ONE buffer of bnn_mx4_bytes(R, K) bytes, 16-byte aligned, with C = ceil(K / 128) chunks per row:
+ *   - codes, [R][64 C] bytes: element k is byte k / 2, the low half for even k;
+ *   - from the next multiple of 256 bytes on the scale bytes, as words [C][R]: byte b of word (c, r) belongs to block 4 c + b of
+ *     row r.
+ * Codes and scale bytes of elements past K are 0; every producer here writes them, every consumer assumes them.
+ * Training uses the same product three times: the layer X W^T, and backward the gradient of its input, G W (rows of G against columns of W), and
+ * of its weights, G^T X (columns against columns).  Sums run along the blocks, so a matrix is needed along its rows, its columns
+ * or both ways.
+ * ---------------------------------------------------------------------------------------------------------------- */
+
+/* Bytes of a matrix [R][K] in the format above; 0 if R or K is not in 1 .. 2^30.  HOST helper. */
+size_t bnn_mx4_bytes(int64_t R, int64_t K);
+
+typedef enum bnn_rounding {
+    BNN_ROUND_NEAREST = 0,    /* the nearest number of the format, of two equally near ones the one with the even code         */
+    BNN_ROUND_STOCHASTIC = 1  /* one of the two neighbours, with the probabilities (to 2^-16) that make the mean right: for gradients */
+} bnn_rounding;
+
+/* From fp32 to 4 bits: X [R][C] along its rows (Q: a matrix [R][C]), along its columns (QT: X^T, a matrix [C][R]) or both, from one read.
+ *   Q, QT  out, nullable, not both NULL
+ *   seed   of the random bits of BNN_ROUND_STOCHASTIC (unused otherwise): the same seed gives the same codes.  Element (r, c) takes
+ *          h = mix(mix(key + r) + c), key = mix(mix(seed % 2^32) + seed / 2^32), its lower 16 bits for Q and its upper 16 for QT
+ *          (mix: x ^= x >> 16, x *= 0x6A09E667, x ^= x >> 15, x *= 0xBB67AE85, x ^= x >> 16, in 32 bits)
+ * A block's scale byte is the smallest with all its numbers within 6 times the scale (nothing is cut off, so that stochastic rounding
+ * has no bias); a block with an Inf or a NaN gets 255 and codes of 0. */
+int bnn_quantize_mx4(const float* X, int64_t R, int64_t C, int rounding, uint64_t seed, void* Q, void* QT, void* stream);
+
+/* The numbers that a matrix [R][K] of that format holds, exactly (but for those below 2^-126 in size, which fp32 has no more bits for): X out, fp32 [R][K]. */
+int bnn_dequantize_mx4(const void* Q, int64_t R, int64_t K, float* X, void* stream);
+
+/* One layer of 4-bit weights on 4-bit inputs: h^[m][n] = sum_k x[m][k] w[n][k] + bias[n], then the activation.  The sum is taken
+ * in fp32 on the matrix cores, in no documented order; products that are below 2^-126 in size may count as 0.
+ *   Xq     a matrix [M][K];  Wq: a matrix [N][K];  bias fp32 [N] or NULL
+ *   act    LINEAR, HARDTANH, SIGMOID, LOGSOFTMAX -> Y fp32 [M][N];  SIGN -> Y words [M][bnn_packed_words(N, word_bits)]
+ *   K is at most 2^22 (BNN_ESHAPE beyond).  Errors as bnn_layer_realw. */
+int bnn_layer_mx4(const void* Xq, const void* Wq, const float* bias, int64_t M, int64_t K, int64_t N, int act, int word_bits, void* Y,
+                  void* stream);
+
+/* The same on fp32 inputs X [M][K], which the call rounds to 4 bits (nearest, blocks along k): the results of bnn_quantize_mx4 and
+ * bnn_layer_mx4.
+ *   workspace  DEVICE scratch of at least bnn_layer_mx4_realx_workspace_bytes(M, K, N) bytes, 256-byte aligned, overlapping none of
+ *              the operands (BNN_EWORKSPACE, BNN_EALIGN, BNN_EINVAL); its contents mean nothing between calls.  The size helper returns 0
+ *              for M = 0 and for shapes the call refuses.  HOST helper. */
+size_t bnn_layer_mx4_realx_workspace_bytes(int64_t M, int64_t K, int64_t N);
+int bnn_layer_mx4_realx(const float* X, const void* Wq, const float* bias, int64_t M, int64_t K, int64_t N, int act, int word_bits, void* Y,
+                        void* workspace, size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------------------------------------------------
+ * AdamW: an update with running means of the gradient and of its square, over all tensors of a network in one launch per 40 of
+ * them.  The states take 8 bytes per element, or 2.06 with state_bits = 8.
+ * ---------------------------------------------------------------------------------------------------------------- */
+
+/* A tensor to update.  HOST struct; the pointers are DEVICE pointers.  A tensor of no elements is skipped, its pointers unread. */
+typedef struct bnn_adamw_tensor {
+    float* w;               /* in/out [count]                                                                      */
+    const float* g;         /* gradient [count]                                                                     */
+    void* m;                /* in/out: state_bits 32: fp32 [count]; 8: signed bytes [count]                         */
+    void* v;                /* in/out: state_bits 32: fp32 [count]; 8: unsigned bytes [count], codes of sqrt(v)     */
+    uint8_t* m_scale;       /* in/out, state_bits 8 only: scale bytes of the blocks of 32 elements, [ceil(count / 32)] */
+    uint8_t* v_scale;
+    int64_t count;          /* at most 2^35                                                                         */
+    int32_t clip;           /* 1: w is clipped to [-1, +1] afterwards (Alg. 1's Clip, for binarised weights); 0: not */
+    int32_t reserved;
+} bnn_adamw_tensor;
+
+/* HOST struct.  A captured graph replays the values it was captured with, but for those that lr_at and step_at point to. */
+typedef struct bnn_adamw_params {
+    double lr, beta1, beta2, eps, weight_decay;   /* lr, weight_decay >= 0; 0 <= beta < 1; eps > 0 in fp32 too            */
+    int64_t step;           /* number of this update, from 1                                                        */
+    int32_t state_bits;     /* 32 or 8                                                                               */
+    int32_t reserved;
+    uint64_t seed;          /* state_bits 8: of the random bits; another one for every step                         */
+    const float* lr_at;     /* DEVICE, nullable: the learning rate is read there when the update runs               */
+    const int64_t* step_at; /* DEVICE, nullable: so is the step's number (below 1 counts as 1)                      */
+} bnn_adamw_params;
+
+/* One update of every tensor.  With t the step, in fp32 with every operation rounded:
+ *     m <- beta1 m + (1 - beta1) g        v <- beta2 v + ((1 - beta2) g) g
+ *     w <- w - ((lr weight_decay) w + (lr / (1 - beta1^t) m) / (sqrt(v) (1 / sqrt(1 - beta2^t)) + eps)),   then Clip if asked for
+ * (the factors in brackets of hyperparameters only are computed in fp64 and rounded once).  States start as zeros, in 8 bits all bytes 0.
+ * state_bits 8: a block's scale stands for 2^(e - 127), the smallest that keeps the block's |m| within 127 times it, its sqrt(v) within
+ * 255 times; a code is the whole part of |number| / scale + u, with u one of 2^16 equally likely steps in [0, 1): right in the mean, so that
+ * beta2 near 1, which moves v by less than half a code per step, still moves it.  The w of a step comes from m and v before that rounding.
+ * u comes from h = mix(mix(key_i + j / 32) + j % 32) for element j of the i-th tensor with elements of the list, from 0,
+ * key_i = mix(mix(mix(seed % 2^32) + seed / 2^32) + i), mix as for bnn_quantize_mx4: its lower 16 bits for m, its upper 16 for v.
+ * An Inf or NaN in a gradient makes the element's w and states NaN or Inf, with 8 bits the states of its block NaN.
+ *   tensors  HOST array of n_tensors.  What a launch writes must overlap nothing else it reads or writes (BNN_EINVAL). */
+int bnn_update_adamw(const bnn_adamw_tensor* tensors, int n_tensors, const bnn_adamw_params* params, void* stream);
+
+/* 8-bit states as the numbers they stand for, for checkpoints or to go on with 32 bits: m_out[i] and v_out[i], fp32 [count] each (v, not
+ * its root).  Of the tensors m, v, m_scale, v_scale and count are read.
+ *   m_out, v_out  HOST arrays of n_tensors DEVICE pointers; either array may be NULL, and any pointer in them. */
+int bnn_unpack_adamw_states(const bnn_adamw_tensor* tensors, int n_tensors, float* const* m_out, float* const* v_out, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1,0 +1,162 @@
+"""Plain numpy definitions of the 4-bit format, of its product and of the AdamW update (test infrastructure only): values in
+64 bits, roundings by comparison with the format's own numbers, 32-bit roundings where the definition fixes them."""
+from __future__ import annotations
+
+import numpy as np
+
+E2M1 = np.array([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0])
+NEAREST, STOCHASTIC = 0, 1
+
+
+def mix(x):
+    x = np.asarray(x, dtype=np.uint32).copy()
+    with np.errstate(over="ignore"):
+        x ^= x >> np.uint32(16)
+        x *= np.uint32(0x6A09E667)
+        x ^= x >> np.uint32(15)
+        x *= np.uint32(0xBB67AE85)
+        x ^= x >> np.uint32(16)
+    return x
+
+
+def _add(a, b):
+    return ((np.asarray(a, np.uint64) + np.asarray(b, np.uint64)) & np.uint64(0xFFFFFFFF)).astype(np.uint32)
+
+
+def seed_key(seed):
+    return mix(_add(mix(seed & 0xFFFFFFFF), seed >> 32))
+
+
+def draws(R, C, seed):
+    """h [R][C] of element (r, c)."""
+    row = mix(_add(seed_key(seed), np.arange(R)))
+    return mix(_add(row[:, None], np.arange(C)[None, :]))
+
+
+def scale_bytes(x, largest):
+    """x [..., 32] -> smallest e in 0 .. 254 with max |x| <= largest 2^(e - 127); 255 where a number is none."""
+    bad = ~np.isfinite(x).all(-1)
+    top = np.where(bad, 0.0, np.abs(np.where(np.isfinite(x), x, 0.0)).max(-1).astype(np.float64))
+    e = np.zeros(top.shape, np.int64)
+    some = top > 0
+    guess = np.zeros(top.shape, np.int64)
+    guess[some] = np.floor(np.log2(top[some])).astype(np.int64) - 9 + 127
+    guess = np.maximum(guess, 0)
+    for _ in range(16):   # up until it holds
+        guess = np.where(top > largest * np.ldexp(1.0, guess - 127), guess + 1, guess)
+    e = np.where(some, guess, 0)
+    assert (top <= largest * np.ldexp(1.0, e - 127)).all()
+    assert ((e == 0) | (top > largest * np.ldexp(1.0, e - 128))).all()
+    return np.where(bad, 255, e)
+
+
+def _blocks(X):
+    R, K = X.shape
+    out = np.zeros((R, (K + 127) // 128 * 128))
+    out[:, :K] = X
+    return out.reshape(R, -1, 32)
+
+
+def quantize(X, rounding=NEAREST, u=None):
+    """X [R][K] -> codes [R][K'] (0 .. 15) and scale bytes [R][K' / 32], K' = K rounded up to 128.  u: draws in [0, 1), [R][K]."""
+    neg = np.signbit(X)
+    x = _blocks(np.asarray(X, np.float64))
+    e = scale_bytes(x, 6.0)
+    with np.errstate(invalid="ignore"):
+        a = np.abs(x) * np.ldexp(1.0, 127 - e)[..., None]
+    a = np.where((e == 255)[..., None], 0.0, a)
+    low = np.searchsorted(E2M1, a, side="right") - 1
+    up = np.minimum(low + 1, 7)
+    gap = np.where(up > low, E2M1[up] - E2M1[low], 1.0)
+    beyond = (a - E2M1[low]) / gap
+    if rounding == NEAREST:
+        take = (beyond > 0.5) | ((beyond == 0.5) & (low % 2 == 1))
+    else:
+        take = beyond + _blocks(u) >= 1.0
+    code = np.where(take, up, low)
+    sign = np.zeros((x.shape[0], x.shape[1] * 32), bool)
+    sign[:, :X.shape[1]] = neg
+    code = np.where((e == 255)[..., None], 0, code | (sign.reshape(x.shape) << 3))
+    return code.reshape(X.shape[0], -1), e
+
+
+def pack(codes, e):
+    R, K = codes.shape
+    c = codes.astype(np.uint8).reshape(R, K // 2, 2)
+    low = (c[:, :, 0] | (c[:, :, 1] << 4)).reshape(-1)
+    words = e.astype(np.uint8).reshape(R, K // 128, 4).transpose(1, 0, 2).reshape(-1)
+    return np.concatenate([low, np.zeros(-low.size % 256, np.uint8), words])
+
+
+def unpack(buf, R, K):
+    """Values, float64 [R][K], of a packed matrix."""
+    C = (K + 127) // 128
+    n = R * C * 64
+    b = buf[:n].reshape(R, C * 64)
+    codes = np.stack([b & 15, b >> 4], 2).reshape(R, C * 128)
+    e = buf[(n + 255) // 256 * 256:].reshape(C, R, 4).transpose(1, 0, 2).reshape(R, C * 4).astype(np.int64)
+    v = np.where(codes & 8, -1.0, 1.0) * E2M1[codes & 7]
+    v = v.reshape(R, -1, 32) * np.where(e == 255, np.nan, np.ldexp(1.0, e - 127))[..., None]
+    return v.reshape(R, -1)[:, :K]
+
+
+def quantized(X, rounding=NEAREST, seed=0, columns=False):
+    """The packed matrix of X [R][C] along its rows, or of X^T."""
+    h = draws(*X.shape, seed)
+    u = ((h >> 16) if columns else (h & 0xFFFF)) / 65536.0
+    return pack(*(quantize(X.T, rounding, u.T) if columns else quantize(X, rounding, u)))
+
+
+def power(beta, t):
+    p = 1.0
+    while t > 0:
+        if t & 1:
+            p *= beta
+        t >>= 1
+        beta *= beta
+    return p
+
+
+def adamw_state(x, largest, h16):
+    """fp32 numbers [n] -> 8-bit codes and scale bytes."""
+    n = x.size
+    x = np.concatenate([x, np.zeros(-n % 32, np.float32)]).reshape(-1, 32)
+    e = scale_bytes(x.astype(np.float64), largest)
+    with np.errstate(invalid="ignore"):
+        y = (np.abs(x.astype(np.float64)) * np.ldexp(1.0, 127 - e)[:, None]).astype(np.float32)
+    y = np.where((e == 255)[:, None], np.float32(0), y)
+    code = np.floor(y + (h16 / np.float32(65536.0)).astype(np.float32)).astype(np.int64)   # (one fp32 addition)
+    return np.where(x < 0, -code, code).reshape(-1)[:n], e.astype(np.uint8)
+
+
+def adamw_decode(codes, e):
+    s = np.where(e == 255, np.nan, np.ldexp(1.0, e.astype(np.int64) - 127)).repeat(32)[:codes.size]
+    return (codes.astype(np.float64) * s).astype(np.float32)
+
+
+def adamw(w, g, m, v, step, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.01, clip=False):
+    """fp32 with every operation rounded; returns w, m, v, sqrt(v)."""
+    f = np.float32
+    b1, c1, b2, c2 = f(beta1), f(1.0 - beta1), f(beta2), f(1.0 - beta2)
+    decay, size = f(lr * weight_decay), f(lr / (1.0 - power(beta1, step)))
+    q = f(1.0 / np.sqrt(1.0 - power(beta2, step)))
+    with np.errstate(all="ignore"):
+        m = b1 * m + c1 * g
+        v = b2 * v + (c2 * g) * g
+        r = np.sqrt(v)
+        w = w - (decay * w + (size * m) / (r * q + f(eps)))
+    if clip:
+        w = np.where(w > 1, f(1), np.where(w < -1, f(-1), w))
+    return w, m, v, r
+
+
+def adamw8(w, g, m, m_scale, v, v_scale, step, seed, index, **kw):
+    """One tensor with 8-bit states: returns w and the new codes and scale bytes."""
+    root = adamw_decode(v, v_scale)
+    w, m2, _, r = adamw(w, g, adamw_decode(m, m_scale), root * root, step, **kw)
+    key = mix(_add(mix(_add(mix(seed & 0xFFFFFFFF), seed >> 32)), index))
+    blocks = (w.size + 31) // 32
+    h = mix(_add(mix(_add(key, np.arange(blocks)))[:, None], np.arange(32)[None, :]))
+    cm, em = adamw_state(m2, 127.0, (h & 0xFFFF).astype(np.float32))
+    cv, ev = adamw_state(r, 255.0, (h >> 16).astype(np.float32))
+    return w, cm.astype(np.int8), em, cv.astype(np.uint8), ev

@@ -9,7 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from ctypes import c_char_p, c_float, c_int, c_int32, c_int64, c_size_t, c_void_p
+from ctypes import c_char_p, c_double, c_float, c_int, c_int32, c_int64, c_size_t, c_uint64, c_void_p
 from typing import Sequence
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -30,6 +30,7 @@ BNN_OPT_COOPERATIVE_SPIN = 15
 BNN_OPT_REALX_I8_LOGSOFTMAX = 16
 BNN_OPT_REALW_SPLIT_LOGSOFTMAX = 17
 BNN_OPT_REALW_VALU_LDS = 18
+BNN_ROUND_NEAREST, BNN_ROUND_STOCHASTIC = 0, 1
 
 ACT_BY_NAME = {"raw": BNN_ACT_RAW_I32, "linear": BNN_ACT_LINEAR, "hardtanh": BNN_ACT_HARDTANH,
                "sign": BNN_ACT_SIGN, "step01": BNN_ACT_SIGN, "logsoftmax": BNN_ACT_LOGSOFTMAX,
@@ -40,6 +41,17 @@ class bnn_layer_desc(ctypes.Structure):
     _fields_ = [("K", c_int64), ("N", c_int64), ("act", c_int32), ("word_bits", c_int32),
                 ("x_is_binary", c_int32), ("w_is_real", c_int32),
                 ("Wp", c_void_p), ("scale", c_void_p), ("bias", c_void_p)]
+
+
+class bnn_adamw_tensor(ctypes.Structure):
+    _fields_ = [("w", c_void_p), ("g", c_void_p), ("m", c_void_p), ("v", c_void_p), ("m_scale", c_void_p),
+                ("v_scale", c_void_p), ("count", c_int64), ("clip", c_int32), ("reserved", c_int32)]
+
+
+class bnn_adamw_params(ctypes.Structure):
+    _fields_ = [("lr", c_double), ("beta1", c_double), ("beta2", c_double), ("eps", c_double), ("weight_decay", c_double),
+                ("step", c_int64), ("state_bits", c_int32), ("reserved", c_int32), ("seed", c_uint64), ("lr_at", c_void_p),
+                ("step_at", c_void_p)]
 
 
 if not os.path.exists(LIB_PATH):
@@ -83,6 +95,15 @@ _SIGNATURES = {
     "bnn_subtract_log_prior": (c_int, [c_void_p, c_void_p, c_int64, c_int64, c_void_p]),
     "bnn_forward_workspace_bytes": (c_size_t, [c_void_p, c_int, c_int64]),
     "bnn_forward": (c_int, [c_void_p, c_int, c_void_p, c_int64, c_void_p, c_void_p, c_size_t, c_void_p]),
+    "bnn_mx4_bytes": (c_size_t, [c_int64, c_int64]),
+    "bnn_quantize_mx4": (c_int, [c_void_p, c_int64, c_int64, c_int, c_uint64, c_void_p, c_void_p, c_void_p]),
+    "bnn_dequantize_mx4": (c_int, [c_void_p, c_int64, c_int64, c_void_p, c_void_p]),
+    "bnn_layer_mx4": (c_int, [c_void_p, c_void_p, c_void_p, c_int64, c_int64, c_int64, c_int, c_int, c_void_p, c_void_p]),
+    "bnn_layer_mx4_realx_workspace_bytes": (c_size_t, [c_int64, c_int64, c_int64]),
+    "bnn_layer_mx4_realx": (c_int, [c_void_p, c_void_p, c_void_p, c_int64, c_int64, c_int64, c_int, c_int, c_void_p, c_void_p,
+                            c_size_t, c_void_p]),
+    "bnn_update_adamw": (c_int, [c_void_p, c_int, c_void_p, c_void_p]),
+    "bnn_unpack_adamw_states": (c_int, [c_void_p, c_int, c_void_p, c_void_p, c_void_p]),
     "bnn_forward_static": (c_int, [c_void_p, c_int, c_void_p, c_int64, c_void_p, c_void_p]),
 }
 for _name, (_res, _args) in _SIGNATURES.items():
@@ -230,6 +251,57 @@ def bnn_subtract_log_prior(logp: int, log_prior: int, M: int, N: int, stream: in
 
 def bnn_semi_stochastic_binarize(w: int, u: int, count: int, stream: int = 0) -> int:
     return _check(_lib.bnn_semi_stochastic_binarize(w, u, count, stream or None))
+
+
+# ---- 4-bit layers and AdamW (argument order as in include/bnn.h)
+
+def bnn_mx4_bytes(R: int, K: int) -> int:
+    return int(_lib.bnn_mx4_bytes(R, K))
+
+
+def bnn_quantize_mx4(X: int, R: int, C: int, rounding: int, seed: int, Q: int, QT: int, stream: int = 0) -> int:
+    return _check(_lib.bnn_quantize_mx4(X, R, C, rounding, seed, Q or None, QT or None, stream or None))
+
+
+def bnn_dequantize_mx4(Q: int, R: int, K: int, X: int, stream: int = 0) -> int:
+    return _check(_lib.bnn_dequantize_mx4(Q, R, K, X, stream or None))
+
+
+def bnn_layer_mx4(Xq: int, Wq: int, bias: int, M: int, K: int, N: int, act: int, word_bits: int, Y: int, stream: int = 0) -> int:
+    return _check(_lib.bnn_layer_mx4(Xq, Wq, bias or None, M, K, N, act, word_bits, Y, stream or None))
+
+
+def bnn_layer_mx4_realx_workspace_bytes(M: int, K: int, N: int) -> int:
+    return int(_lib.bnn_layer_mx4_realx_workspace_bytes(M, K, N))
+
+
+def bnn_layer_mx4_realx(X: int, Wq: int, bias: int, M: int, K: int, N: int, act: int, word_bits: int, Y: int, workspace: int,
+                        workspace_bytes: int, stream: int = 0) -> int:
+    return _check(_lib.bnn_layer_mx4_realx(X, Wq, bias or None, M, K, N, act, word_bits, Y, workspace or None, workspace_bytes,
+                                           stream or None))
+
+
+def make_adamw_array(descs: Sequence[dict]):
+    """HOST array of bnn_adamw_tensor from dicts with keys w, g, m, v, count and, optionally, m_scale, v_scale and clip."""
+    arr = (bnn_adamw_tensor * len(descs))()
+    for i, d in enumerate(descs):
+        for name in ("w", "g", "m", "v", "m_scale", "v_scale"):
+            setattr(arr[i], name, d.get(name) or None)
+        arr[i].count, arr[i].clip = d["count"], int(d.get("clip", 0))
+    return arr
+
+
+def make_pointer_array(pointers: Sequence[int]):
+    """HOST array of device pointers (0 = NULL)."""
+    return (c_void_p * len(pointers))(*[p or None for p in pointers])
+
+
+def bnn_update_adamw(tensors, n_tensors: int, params, stream: int = 0) -> int:
+    return _check(_lib.bnn_update_adamw(tensors, n_tensors, ctypes.byref(params) if params is not None else None, stream or None))
+
+
+def bnn_unpack_adamw_states(tensors, n_tensors: int, m_out, v_out, stream: int = 0) -> int:
+    return _check(_lib.bnn_unpack_adamw_states(tensors, n_tensors, m_out or None, v_out or None, stream or None))
 
 
 def make_layer_array(descs: Sequence[dict]):

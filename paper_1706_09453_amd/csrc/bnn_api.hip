@@ -25,8 +25,6 @@
 #include "train_kernels.hpp"
 #include "valu_kernels.hpp"
 
-#define BNN_EXPORT extern "C" __attribute__((visibility("default")))
-
 // Hand-over area of the cooperative log-Softmax epilogue (BNN_OPT_COOPERATIVE): a fixed array in the library's device
 // image, kCoopSlots launches' worth, handed out round-robin, so that the tail of one launch and the head of the next
 // on another stream do not share a slot.  In host code the array's name is only a handle for hipGetSymbolAddress.
@@ -36,6 +34,18 @@ constexpr size_t kCoopFlagBytes = (size_t)kCoopMaxTiles * 8;
 constexpr size_t kCoopPairBytes = (size_t)kCoopMaxTiles * 256 * 8;         // 256 rows per tile, 8 bytes per (max, sum) pair
 constexpr size_t kCoopSlotBytes = kCoopFlagBytes + kCoopPairBytes;
 static __device__ __align__(256) unsigned char coop_area[256 + kCoopSlots * kCoopSlotBytes];   // [0, 4): timeouts
+
+namespace bnn {
+void launch_log_softmax(float* Z, int M, int N, hipStream_t st) {
+    const dim3 grid(M < 65536 ? M : 65536), block(256);
+    const bool al = aligned(Z, 16);
+    if (al && N <= 1024) log_softmax_rows_reg_kernel<4><<<grid, block, 0, st>>>(Z, M, N);
+    else if (al && N <= 2048) log_softmax_rows_reg_kernel<8><<<grid, block, 0, st>>>(Z, M, N);
+    else if (al && N <= 4096) log_softmax_rows_reg_kernel<16><<<grid, block, 0, st>>>(Z, M, N);
+    else if (al && N <= 8192) log_softmax_rows_reg_kernel<32><<<grid, block, 0, st>>>(Z, M, N);
+    else log_softmax_rows_kernel<<<grid, block, 0, st>>>(Z, M, N);
+}
+}  // namespace bnn
 
 namespace {
 
@@ -81,19 +91,6 @@ unsigned char* coop_base(int* dev_out) {
     g_coop_ptr[dev].store(p, std::memory_order_release);
     return static_cast<unsigned char*>(p);
 }
-
-inline bool word_bits_ok(int wb) { return wb == 32 || wb == 64; }
-inline int64_t words_per_row(int64_t K, int wb) { return (K + wb - 1) / wb; }
-// Row length in 32-bit words (a 64-bit word is two little-endian 32-bit words).
-inline int64_t row_w32(int64_t K, int wb) { return words_per_row(K, wb) * (wb / 32); }
-inline bool overlap(const void* a, size_t na, const void* b, size_t nb) {
-    const uintptr_t a0 = reinterpret_cast<uintptr_t>(a), b0 = reinterpret_cast<uintptr_t>(b);
-    return na && nb && a0 < b0 + nb && b0 < a0 + na;
-}
-inline int launch_status() { return hipGetLastError() == hipSuccess ? BNN_OK : BNN_EDEVICE; }
-
-constexpr int64_t kMaxDim = (int64_t)1 << 30;
-constexpr int64_t kMaxN = (int64_t)1 << 22;   // outputs of a layer: the second grid dimension (65535) counts tiles of 128 or 256 of them
 
 size_t out_bytes(int64_t M, int64_t N, int act, int wb) {
     if (act == BNN_ACT_SIGN) return (size_t)M * (size_t)row_w32(N, wb) * 4;
@@ -193,16 +190,6 @@ void launch_realx_tm(const float* X, const uint32_t* Wp, const float* scale, con
                      int w32, int act, void* Y, int yw32, hipStream_t st, Front* front) {
     if ((K & 3) == 0 && aligned(X, 16)) launch_realx_tm_b<TM, true>(X, Wp, scale, bias, M, K, N, w32, act, Y, yw32, st, front);
     else launch_realx_tm_b<TM, false>(X, Wp, scale, bias, M, K, N, w32, act, Y, yw32, st, front);
-}
-
-void launch_log_softmax(float* Z, int M, int N, hipStream_t st) {
-    const dim3 grid(M < 65536 ? M : 65536), block(256);
-    const bool al = aligned(Z, 16);
-    if (al && N <= 1024) log_softmax_rows_reg_kernel<4><<<grid, block, 0, st>>>(Z, M, N);
-    else if (al && N <= 2048) log_softmax_rows_reg_kernel<8><<<grid, block, 0, st>>>(Z, M, N);
-    else if (al && N <= 4096) log_softmax_rows_reg_kernel<16><<<grid, block, 0, st>>>(Z, M, N);
-    else if (al && N <= 8192) log_softmax_rows_reg_kernel<32><<<grid, block, 0, st>>>(Z, M, N);
-    else log_softmax_rows_kernel<<<grid, block, 0, st>>>(Z, M, N);
 }
 
 int run_realx(const float* X, const void* Wp, const float* scale, const float* bias, int64_t M, int64_t K, int64_t N,

@@ -1,0 +1,121 @@
+// C ABI of the 4-bit layers: argument checks, kernel selection, launches.
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+#include "../../include/bnn.h"
+#include "launch.hpp"
+#include "mx4_gemm_kernels.hpp"
+#include "mx4_kernels.hpp"
+
+namespace {
+
+using namespace bnn;
+
+constexpr int64_t kMx4MaxK = (int64_t)1 << 22;
+
+bool mx4_dims_ok(int64_t R, int64_t K) { return R > 0 && K > 0 && R <= kMaxDim && K <= kMaxDim; }
+
+int run_quantize(const float* X, int64_t R, int64_t C, int rounding, uint64_t seed, void* Q, void* QT, hipStream_t st) {
+    const int tr = (int)((R + 127) / 128), tc = (int)((C + 127) / 128);
+    const int64_t tiles = (int64_t)tr * tc;
+    const dim3 grid((unsigned)(tiles < 65536 ? tiles : 65536));
+    const bool vec = C % 4 == 0 && aligned(X, 16), stochastic = rounding == BNN_ROUND_STOCHASTIC;
+    const uint32_t key = seed_key(seed);
+    auto go = [&](auto v, auto s) {
+        mx4_quantize_kernel<decltype(v)::value, decltype(s)::value><<<grid, 256, 0, st>>>(X, (int)R, (int)C, key, Q, QT, tr, tc);
+    };
+    if (vec && stochastic) go(std::true_type{}, std::true_type{});
+    else if (vec) go(std::true_type{}, std::false_type{});
+    else if (stochastic) go(std::false_type{}, std::true_type{});
+    else go(std::false_type{}, std::false_type{});
+    return launch_status();
+}
+
+int run_layer(const void* Xq, const void* Wq, const float* bias, int64_t M, int64_t K, int64_t N, int act, int wb, void* Y, hipStream_t st) {
+    const int chunks = (int)mx4_chunks(K), yw32 = (int)row_w32(N, wb);
+    const dim3 grid((unsigned)((M + 127) / 128), (unsigned)((N + 127) / 128));
+    auto go = [&](auto a) {
+        mx4_gemm_simple_kernel<decltype(a)::value><<<grid, 256, 0, st>>>(Xq, Wq, bias, (int)M, (int)K, (int)N, chunks, Y, yw32);
+    };
+    switch (act) {
+        case BNN_ACT_SIGN: go(std::integral_constant<int, ACT_SIGN>{}); break;
+        case BNN_ACT_HARDTANH: go(std::integral_constant<int, ACT_HARDTANH>{}); break;
+        case BNN_ACT_SIGMOID: go(std::integral_constant<int, ACT_SIGMOID>{}); break;
+        default: go(std::integral_constant<int, ACT_LINEAR>{}); break;
+    }
+    if (act == BNN_ACT_LOGSOFTMAX) launch_log_softmax(static_cast<float*>(Y), (int)M, (int)N, st);
+    return launch_status();
+}
+
+// What both layer calls ask of their arguments; X: 4-bit codes or fp32 (`real`).
+int check_layer(const void* X, bool real, const void* Wq, const float* bias, int64_t M, int64_t K, int64_t N, int act, int wb, const void* Y) {
+    if (!word_bits_ok(wb) || M < 0 || K <= 0 || N <= 0 || M > kMaxDim || K > kMx4MaxK || N > kMaxN) return BNN_ESHAPE;
+    if (act <= BNN_ACT_RAW_I32 || act > BNN_ACT_SIGMOID) return BNN_EINVAL;
+    if (M == 0) return BNN_OK;
+    if (!X || !Wq || !Y) return BNN_EINVAL;
+    if (!aligned(Wq, 16) || !aligned(X, real ? 4 : 16) || !aligned(bias, 4)) return BNN_EALIGN;
+    if (!aligned(Y, act == BNN_ACT_SIGN ? wb / 8 : 4)) return BNN_EALIGN;
+    const size_t yb = act == BNN_ACT_SIGN ? (size_t)M * (size_t)row_w32(N, wb) * 4 : (size_t)M * (size_t)N * 4;
+    if (overlap(X, real ? (size_t)M * (size_t)K * 4 : mx4_bytes(M, K), Y, yb) || overlap(Wq, mx4_bytes(N, K), Y, yb)) return BNN_EINVAL;
+    if (bias && overlap(bias, (size_t)N * 4, Y, yb)) return BNN_EINVAL;
+    return BNN_OK;
+}
+
+}  // namespace
+
+BNN_EXPORT size_t bnn_mx4_bytes(int64_t R, int64_t K) { return mx4_dims_ok(R, K) ? mx4_bytes(R, K) : 0; }
+
+BNN_EXPORT int bnn_quantize_mx4(const float* X, int64_t R, int64_t C, int rounding, uint64_t seed, void* Q, void* QT, void* stream) {
+    if (R < 0 || C <= 0 || R > kMaxDim || C > kMaxDim) return BNN_ESHAPE;
+    if (rounding != BNN_ROUND_NEAREST && rounding != BNN_ROUND_STOCHASTIC) return BNN_EINVAL;
+    if (R == 0) return BNN_OK;
+    if (!X || (!Q && !QT)) return BNN_EINVAL;
+    if (!aligned(X, 4) || !aligned(Q, 16) || !aligned(QT, 16)) return BNN_EALIGN;
+    const size_t xb = (size_t)R * (size_t)C * 4, qb = Q ? mx4_bytes(R, C) : 0, tb = QT ? mx4_bytes(C, R) : 0;
+    if (overlap(X, xb, Q, qb) || overlap(X, xb, QT, tb) || overlap(Q, qb, QT, tb)) return BNN_EINVAL;
+    return run_quantize(X, R, C, rounding, seed, Q, QT, static_cast<hipStream_t>(stream));
+}
+
+BNN_EXPORT int bnn_dequantize_mx4(const void* Q, int64_t R, int64_t K, float* X, void* stream) {
+    if (R < 0 || K <= 0 || R > kMaxDim || K > kMaxDim) return BNN_ESHAPE;
+    if (R == 0) return BNN_OK;
+    if (!Q || !X) return BNN_EINVAL;
+    if (!aligned(Q, 16) || !aligned(X, 4)) return BNN_EALIGN;
+    if (overlap(Q, mx4_bytes(R, K), X, (size_t)R * (size_t)K * 4)) return BNN_EINVAL;
+    const int chunks = (int)mx4_chunks(K);
+    const int64_t blocks = (R * chunks * 32 + 255) / 256;
+    const unsigned grid = (unsigned)(blocks < 65536 ? blocks : 65536);
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    if (K % 4 == 0 && aligned(X, 16)) mx4_dequantize_kernel<true><<<grid, 256, 0, st>>>(Q, (int)R, (int)K, chunks, X);
+    else mx4_dequantize_kernel<false><<<grid, 256, 0, st>>>(Q, (int)R, (int)K, chunks, X);
+    return launch_status();
+}
+
+BNN_EXPORT int bnn_layer_mx4(const void* Xq, const void* Wq, const float* bias, int64_t M, int64_t K, int64_t N, int act, int word_bits, void* Y,
+                             void* stream) {
+    const int rc = check_layer(Xq, false, Wq, bias, M, K, N, act, word_bits, Y);
+    if (rc != BNN_OK || M == 0) return rc;
+    return run_layer(Xq, Wq, bias, M, K, N, act, word_bits, Y, static_cast<hipStream_t>(stream));
+}
+
+BNN_EXPORT size_t bnn_layer_mx4_realx_workspace_bytes(int64_t M, int64_t K, int64_t N) {
+    if (M <= 0 || K <= 0 || N <= 0 || M > kMaxDim || K > kMx4MaxK || N > kMaxN) return 0;
+    return mx4_bytes(M, K);
+}
+
+BNN_EXPORT int bnn_layer_mx4_realx(const float* X, const void* Wq, const float* bias, int64_t M, int64_t K, int64_t N, int act, int word_bits, void* Y,
+                                   void* workspace, size_t workspace_bytes, void* stream) {
+    const int rc = check_layer(X, true, Wq, bias, M, K, N, act, word_bits, Y);
+    if (rc != BNN_OK || M == 0) return rc;
+    const size_t need = mx4_bytes(M, K), xb = (size_t)M * (size_t)K * 4;
+    const size_t yb = act == BNN_ACT_SIGN ? (size_t)M * (size_t)row_w32(N, word_bits) * 4 : (size_t)M * (size_t)N * 4;
+    if (!workspace || workspace_bytes < need) return BNN_EWORKSPACE;
+    if (!aligned(workspace, 256)) return BNN_EALIGN;
+    if (overlap(workspace, need, X, xb) || overlap(workspace, need, Wq, mx4_bytes(N, K)) || overlap(workspace, need, Y, yb) ||
+        (bias && overlap(workspace, need, bias, (size_t)N * 4)))
+        return BNN_EINVAL;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    const int q = run_quantize(X, M, K, BNN_ROUND_NEAREST, 0, workspace, nullptr, st);
+    return q != BNN_OK ? q : run_layer(workspace, Wq, bias, M, K, N, act, word_bits, Y, st);
+}
