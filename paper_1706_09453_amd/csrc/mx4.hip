@@ -1,6 +1,7 @@
 // C ABI of the 4-bit layers: argument checks, kernel selection, launches.
 #include <hip/hip_runtime.h>
 
+#include <atomic>
 #include <cstdint>
 
 #include "../../include/bnn.h"
@@ -16,27 +17,59 @@ constexpr int64_t kMx4MaxK = (int64_t)1 << 22;
 
 bool mx4_dims_ok(int64_t R, int64_t K) { return R > 0 && K > 0 && R <= kMaxDim && K <= kMaxDim; }
 
+template <bool VEC, bool STOCHASTIC>
+void launch_quantize(const float* X, int R, int C, uint32_t key, void* Q, void* QT, hipStream_t st) {
+    const int tr = (R + 127) / 128, tc = (C + 127) / 128;
+    auto grid = [](int64_t n) { return dim3((unsigned)(n < 65536 ? n : 65536)); };
+    if (!QT) {
+        // 16 rows a workgroup while that leaves CUs idle, 32 beyond
+        if ((int64_t)((R + 31) / 32) * tc < 512)
+            mx4_quantize_rows_kernel<VEC, STOCHASTIC, 1><<<grid((int64_t)((R + 15) / 16) * tc), 256, 0, st>>>(X, R, C, key, Q, tc);
+        else
+            mx4_quantize_rows_kernel<VEC, STOCHASTIC, 2><<<grid((int64_t)((R + 31) / 32) * tc), 256, 0, st>>>(X, R, C, key, Q, tc);
+    } else if (!Q) {
+        mx4_quantize_columns_kernel<STOCHASTIC, false><<<grid((int64_t)tr * tc), 256, 0, st>>>(X, R, C, key, Q, QT, tr, tc);
+    } else {
+        mx4_quantize_columns_kernel<STOCHASTIC, true><<<grid((int64_t)tr * tc), 256, 0, st>>>(X, R, C, key, Q, QT, tr, tc);
+    }
+}
 int run_quantize(const float* X, int64_t R, int64_t C, int rounding, uint64_t seed, void* Q, void* QT, hipStream_t st) {
-    const int tr = (int)((R + 127) / 128), tc = (int)((C + 127) / 128);
-    const int64_t tiles = (int64_t)tr * tc;
-    const dim3 grid((unsigned)(tiles < 65536 ? tiles : 65536));
     const bool vec = C % 4 == 0 && aligned(X, 16), stochastic = rounding == BNN_ROUND_STOCHASTIC;
     const uint32_t key = seed_key(seed);
-    auto go = [&](auto v, auto s) {
-        mx4_quantize_kernel<decltype(v)::value, decltype(s)::value><<<grid, 256, 0, st>>>(X, (int)R, (int)C, key, Q, QT, tr, tc);
-    };
-    if (vec && stochastic) go(std::true_type{}, std::true_type{});
-    else if (vec) go(std::true_type{}, std::false_type{});
-    else if (stochastic) go(std::false_type{}, std::true_type{});
-    else go(std::false_type{}, std::false_type{});
+    if (vec && stochastic) launch_quantize<true, true>(X, (int)R, (int)C, key, Q, QT, st);
+    else if (vec) launch_quantize<true, false>(X, (int)R, (int)C, key, Q, QT, st);
+    else if (stochastic) launch_quantize<false, true>(X, (int)R, (int)C, key, Q, QT, st);
+    else launch_quantize<false, false>(X, (int)R, (int)C, key, Q, QT, st);
     return launch_status();
 }
 
+template <int FM, int FN, int WAVES_M, int WAVES_N, int STAGES, int ACT>
+bool launch_gemm(const void* Xq, const void* Wq, const float* bias, int M, int K, int N, void* Y, int yw32, int nt, hipStream_t st) {
+    using T = Mx4Tile<FM, FN, WAVES_M, WAVES_N, STAGES>;
+    const auto kernel = mx4_gemm_kernel<FM, FN, WAVES_M, WAVES_N, STAGES, ACT>;
+    if constexpr (T::kLds > 65536) {
+        static std::atomic<uint64_t> allowed{0};
+        if (!allow_lds(kernel, T::kLds, allowed)) return false;
+    }
+    const dim3 grid((unsigned)((M + T::kRows - 1) / T::kRows), (unsigned)((N + T::kCols - 1) / T::kCols));
+    kernel<<<grid, T::kThreads, T::kLds, st>>>(Xq, Wq, bias, M, K, N, (int)mx4_chunks(K), Y, yw32, nt);
+    return true;
+}
+
 int run_layer(const void* Xq, const void* Wq, const float* bias, int64_t M, int64_t K, int64_t N, int act, int wb, void* Y, hipStream_t st) {
-    const int chunks = (int)mx4_chunks(K), yw32 = (int)row_w32(N, wb);
-    const dim3 grid((unsigned)((M + 127) / 128), (unsigned)((N + 127) / 128));
+    const int yw32 = (int)row_w32(N, wb);
+    const auto tiles = [&](int rows, int cols) { return ((M + rows - 1) / rows) * ((N + cols - 1) / cols); };
+    // Outputs that the caches will not hold, in rows of whole lines, are stored past them: 16384 x 4096 x 4096 190 -> 172 us, 4096 x 2048 x 2048
+    // 16.4 -> 15.4.  (Rows that are no whole lines would leave as pieces of lines: 4096 x 2048 x 3400 25 -> 39 us.)
+    const int nt = act != BNN_ACT_LOGSOFTMAX && N % 32 == 0 && aligned(Y, 128) && M * N >= (int64_t)8 << 20;
+    bool ok = true;
     auto go = [&](auto a) {
-        mx4_gemm_simple_kernel<decltype(a)::value><<<grid, 256, 0, st>>>(Xq, Wq, bias, (int)M, (int)K, (int)N, chunks, Y, yw32);
+        constexpr int A = decltype(a)::value;
+        if (tiles(64, 64) <= 256) ok = launch_gemm<1, 1, 2, 2, 4, A>(Xq, Wq, bias, (int)M, (int)K, (int)N, Y, yw32, nt, st);
+        else if (tiles(128, 64) <= 256) ok = launch_gemm<2, 1, 2, 2, 4, A>(Xq, Wq, bias, (int)M, (int)K, (int)N, Y, yw32, nt, st);
+        else if (tiles(128, 128) <= 512) ok = launch_gemm<2, 2, 2, 2, 3, A>(Xq, Wq, bias, (int)M, (int)K, (int)N, Y, yw32, nt, st);
+        else if (tiles(256, 128) <= 512) ok = launch_gemm<4, 2, 2, 2, 3, A>(Xq, Wq, bias, (int)M, (int)K, (int)N, Y, yw32, nt, st);
+        else ok = launch_gemm<4, 2, 2, 4, 4, A>(Xq, Wq, bias, (int)M, (int)K, (int)N, Y, yw32, nt, st);
     };
     switch (act) {
         case BNN_ACT_SIGN: go(std::integral_constant<int, ACT_SIGN>{}); break;
@@ -44,6 +77,7 @@ int run_layer(const void* Xq, const void* Wq, const float* bias, int64_t M, int6
         case BNN_ACT_SIGMOID: go(std::integral_constant<int, ACT_SIGMOID>{}); break;
         default: go(std::integral_constant<int, ACT_LINEAR>{}); break;
     }
+    if (!ok) return BNN_EDEVICE;
     if (act == BNN_ACT_LOGSOFTMAX) launch_log_softmax(static_cast<float*>(Y), (int)M, (int)N, st);
     return launch_status();
 }

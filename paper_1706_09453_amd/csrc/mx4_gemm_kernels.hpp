@@ -17,69 +17,204 @@ __device__ __forceinline__ float mx4_act(float h) {
     else return h;
 }
 
-// Operand layout: lane (r = lane % 32, g = lane / 32) holds the 32 elements 32 g ... of row r, and their scale byte.
-// A workgroup is 2 x 2 waves of 64 x 64 outputs.  Rows past M and N repeat the last one and are not stored.
-template <int ACT>
-__global__ __launch_bounds__(256) void mx4_gemm_simple_kernel(const void* __restrict__ Xq, const void* __restrict__ Wq, const float* __restrict__ bias,
-                                                              int M, int K, int N, int chunks, void* __restrict__ Y, int yw32) {
+// ---- Batches.  Operand layout of the instruction: lane (r = lane % 32, g = lane / 32) holds 32 elements, one block, of row r: block g of
+// the 64 elements of a step, 16 bytes, and its scale byte.
+// Both operands of a workgroup's tile go to LDS by loads that write it directly, in stages of a chunk (128 elements: 64 bytes of codes and a
+// word of scale bytes per row), STAGES of them in rotation.  In LDS a row's four 16-byte pieces lie at piece ^ (row / 4 % 4), so that the 16
+// lanes that are served together read 16 different places of the 64 banks.
+template <int FM, int FN, int WAVES_M, int WAVES_N, int STAGES>
+struct Mx4Tile {
+    static constexpr int kWaves = WAVES_M * WAVES_N, kThreads = 64 * kWaves;
+    static constexpr int kRows = 32 * FM * WAVES_M, kCols = 32 * FN * WAVES_N;   // frames and outputs of a workgroup
+    static constexpr int kCodes = (kRows + kCols) * 64, kStage = kCodes + (kRows + kCols) * 4;
+    static constexpr unsigned kLds = (unsigned)STAGES * kStage + kCols * 4;   // stages; bias
+    static constexpr int kAL = kRows / 16 / kWaves, kBL = kCols / 16 / kWaves;   // loads of 16 rows per wave and stage
+    static constexpr int kScaleLoads = (kRows + kCols) / 64;                     // loads of 64 scale words per stage, and
+    static constexpr int kSL = (kScaleLoads + kWaves - 1) / kWaves;              // per wave (some twice, so that all waves have as many)
+    static constexpr int kLoads = kAL + kBL + kSL;
+    static_assert(kRows % (16 * kWaves) == 0 && kCols % (16 * kWaves) == 0 && kRows % 64 == 0 && kCols % 64 == 0 && kCols / 64 <= kWaves);
+};
+
+template <int FM, int FN, int WAVES_M, int WAVES_N, int STAGES, int ACT>
+__global__ __launch_bounds__(64 * WAVES_M * WAVES_N, FM * FN > 8 ? 1 : 2) void mx4_gemm_kernel(const void* __restrict__ Xq, const void* __restrict__ Wq,
+                                                                         const float* __restrict__ bias, int M, int K, int N, int chunks,
+                                                                         void* __restrict__ Y, int yw32, int nt) {
+    using T = Mx4Tile<FM, FN, WAVES_M, WAVES_N, STAGES>;
+    extern __shared__ __attribute__((aligned(16))) unsigned char mx4_mem[];
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = lane_id(), r = lane & 31, g = lane >> 5;
-    const int m_base = (int)blockIdx.x * 128 + (wave >> 1) * 64, n_base = (int)blockIdx.y * 128 + (wave & 1) * 64;
-    if (m_base >= M || n_base >= N) return;
-    const unsigned char *xc = static_cast<const unsigned char*>(Xq), *wc = static_cast<const unsigned char*>(Wq);
-    const uint32_t *xs = mx4_scales(Xq, M, K), *ws = mx4_scales(Wq, N, K);
-    v16f acc[2][2];
-    size_t mrow[2], nrow[2];
+    const int wm = wave / WAVES_N, wn = wave % WAVES_N;
+    int tile_m, tile_n;
+    xcd_tile(tile_m, tile_n);
+    const int m0 = tile_m * T::kRows, n0 = tile_n * T::kCols;
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)mx4_mem;
+
+    // ---- the wave's share of a stage's loads: rows in pieces of 16 bytes, four lanes a row; scale words, one lane a row.  Rows past the
+    // last one repeat it.
+    const int row_bytes = chunks * 64;
+    const i32x4m xr = raw_buffer(static_cast<const unsigned char*>(Xq) + (size_t)m0 * row_bytes, 0x7FFFFFFFu);
+    const i32x4m wr = raw_buffer(static_cast<const unsigned char*>(Wq) + (size_t)n0 * row_bytes, 0x7FFFFFFFu);
+    const uint32_t *xs = mx4_scales(Xq, M, K) + m0, *ws = mx4_scales(Wq, N, K) + n0;
+    const int piece = ((lane & 3) ^ ((lane >> 4) & 3)) * 16;
+    int xo[T::kAL], wo[T::kBL], so[T::kSL];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        mrow[i] = (size_t)min(m_base + 32 * i + r, M - 1);
-        nrow[i] = (size_t)min(n_base + 32 * i + r, N - 1);
+    for (int i = 0; i < T::kAL; ++i) xo[i] = min((wave * T::kAL + i) * 16 + (lane >> 2), M - 1 - m0) * row_bytes + piece;
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
+    for (int i = 0; i < T::kBL; ++i) wo[i] = min((wave * T::kBL + i) * 16 + (lane >> 2), N - 1 - n0) * row_bytes + piece;
+#pragma unroll
+    for (int i = 0; i < T::kSL; ++i) {
+        const int row = (wave * T::kSL + i) % T::kScaleLoads * 64 + lane;   // frames rows first: a load has rows of one kind only
+        so[i] = (row < T::kRows ? min(row, M - 1 - m0) : min(row - T::kRows, N - 1 - n0)) * 4;
+    }
+    auto request_one = [&](int l, int c, int slot) {   // load l of the wave's kLoads of stage c
+        const uint32_t base = lds0 + (uint32_t)(slot * T::kStage);
+        if (l < T::kAL) {
+            load_lds16(xr, xo[l], c * 64, base + (uint32_t)((wave * T::kAL + l) * 1024));
+        } else if (l < T::kAL + T::kBL) {
+            const int i = l - T::kAL;
+            load_lds16(wr, wo[i], c * 64, base + (uint32_t)(T::kRows * 64 + (wave * T::kBL + i) * 1024));
+        } else {
+            const int i = l - T::kAL - T::kBL, row = (wave * T::kSL + i) % T::kScaleLoads * 64;
+            const uint32_t* s = row < T::kRows ? xs + (size_t)c * M : ws + (size_t)c * N;
+            load_lds4(raw_buffer(s, 0x7FFFFFFFu), so[i], 0, base + (uint32_t)(T::kCodes + row * 4));
+        }
+    };
+    auto request = [&](int c, int slot) {
+#pragma unroll
+        for (int l = 0; l < T::kLoads; ++l) request_one(l, c, slot);
+    };
+    // the bias of the tile's columns, in front of the first stage
+    if (bias && wave < T::kCols / 64)
+        load_lds4(raw_buffer(bias + n0, 0x7FFFFFFFu), min(wave * 64 + lane, N - 1 - n0) * 4, 0, lds0 + (uint32_t)(STAGES * T::kStage + wave * 256));
+#pragma unroll
+    for (int c = 0; c < STAGES; ++c)
+        if (c < chunks) request(c, c);
+    // One barrier per stage, in its middle: behind it stage c + 1 is complete in LDS and stage c has been read by every wave, so that its
+    // place takes stage c + STAGES.  (lgkmcnt: the wave's own reads of stage c.)  The last STAGES stages wait for all that is on its way.
+    auto turn = [&]() {
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((STAGES - 2) * T::kLoads) : "memory");
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    auto last_turn = [&]() {
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    const int steady = chunks > STAGES ? chunks - STAGES : 0;
+    auto next_slot = [](int s) { return s == STAGES - 1 ? 0 : s + 1; };
+    const int m_base = m0 + wm * (32 * FM), n_base = n0 + wn * (32 * FN);
+    if (STAGES <= chunks) asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"((STAGES - 1) * T::kLoads) : "memory");
+    else asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+    if (m_base >= M || (ACT == ACT_SIGN ? n_base >= 32 * yw32 : n_base >= N)) {   // wave-uniform: nothing to write, but its share of the stages to bring
+        int c = 0;
+        for (int slot = 0; c < steady; ++c, slot = next_slot(slot)) {
+            turn();
+            request(c + STAGES, slot);
+        }
+        for (; c < chunks; ++c) last_turn();
+        return;
+    }
+    v16f acc[FM][FN];
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j)
 #pragma unroll
             for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.0f;
-    }
-    for (int c = 0; c < chunks; ++c) {
-        v8i a[2][2], b[2][2];
-        int sa[2], sb[2];
+    const int arow = wm * (32 * FM) + r, brow = T::kRows + wn * (32 * FN) + r;
+    const int p0 = (g ^ ((r >> 2) & 3)) * 16, p1 = ((2 + g) ^ ((r >> 2) & 3)) * 16;
+    // the lane's blocks of one of a stage's two steps, fragment f of FN + FM, and its scale words
+    auto fetch_one = [&](int f, v8i (&a)[FM], v8i (&b)[FN], int slot, int p) {
+        const unsigned char* st = mx4_mem + slot * T::kStage + p;
+        const int4 q = *reinterpret_cast<const int4*>(st + (f < FN ? brow + 32 * f : arow + 32 * (f - FN)) * 64);
+        (f < FN ? b[f < FN ? f : 0] : a[f < FN ? 0 : f - FN]) = v8i{q.x, q.y, q.z, q.w, 0, 0, 0, 0};
+    };
+    auto fetch_scale = [&](int f, int (&sa)[FM], int (&sb)[FN], int slot) {
+        const unsigned char* st = mx4_mem + slot * T::kStage + T::kCodes;
+        const int q = *reinterpret_cast<const int*>(st + (f < FN ? brow + 32 * f : arow + 32 * (f - FN)) * 4);
+        (f < FN ? sb[f < FN ? f : 0] : sa[f < FN ? 0 : f - FN]) = q;
+    };
+    constexpr int F = FM + FN, P = FM * FN;   // fragments, products of a step
+    v8i a0[FM], b0[FN], a1[FM], b1[FN];
+    int sa[FM], sb[FN], na[FM], nb[FN];
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
+    for (int f = 0; f < F; ++f) fetch_one(f, a0, b0, 0, p0);
 #pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                const int4 p = *reinterpret_cast<const int4*>(xc + (mrow[i] * chunks + c) * 64 + 32 * s + 16 * g);
-                const int4 q = *reinterpret_cast<const int4*>(wc + (nrow[i] * chunks + c) * 64 + 32 * s + 16 * g);
-                a[i][s] = v8i{p.x, p.y, p.z, p.w, 0, 0, 0, 0};
-                b[i][s] = v8i{q.x, q.y, q.z, q.w, 0, 0, 0, 0};
-            }
-            sa[i] = (int)(xs[(size_t)c * M + mrow[i]] >> (8 * g));   // bytes 0 and 2: the lane's block of both steps
-            sb[i] = (int)(ws[(size_t)c * N + nrow[i]] >> (8 * g));
+    for (int f = 0; f < F; ++f) fetch_scale(f, na, nb, 0);
+    int c = 0, slot = 0;
+    // A wave issues in order, and a product that finds the matrix core busy (32 clocks each) holds up what follows it: what else a stage
+    // asks for is spread over the products, a slot behind each, pinned by scheduling barriers.
+    auto stage = [&](auto more) {   // more: stage c + STAGES is requested
+        const int nslot = next_slot(slot);
+#pragma unroll
+        for (int j = 0; j < FN; ++j) sb[j] = nb[j] >> (8 * g);   // bytes 0 and 2: the lane's blocks of the two steps
+#pragma unroll
+        for (int i = 0; i < FM; ++i) sa[i] = na[i] >> (8 * g);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int q = 0; q < P; ++q) {
+            const int i = q / FN, j = q % FN;
+            acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a0[i], b0[j], acc[i][j], 4, 4, 0, sa[i], 0, sb[j]);
+#pragma unroll
+            for (int f = q * F / P; f < (q + 1) * F / P; ++f) fetch_one(f, a1, b1, slot, p1);
+            __builtin_amdgcn_sched_barrier(0);
         }
+        if constexpr (decltype(more)::value) turn();
+        else last_turn();
+        const int from = decltype(more)::value || c + 1 < chunks ? nslot : slot;   // (behind the last stage: read again, unused)
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int q = 0; q < P; ++q) {
+            const int i = q / FN, j = q % FN;
+            acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a1[i], b1[j], acc[i][j], 4, 4, 2, sa[i], 2, sb[j]);
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a[i][0], b[j][0], acc[i][j], 4, 4, 0, sa[i], 0, sb[j]);
-                acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a[i][1], b[j][1], acc[i][j], 4, 4, 2, sa[i], 2, sb[j]);
+            for (int f = q * F / P; f < (q + 1) * F / P; ++f) {
+                fetch_one(f, a0, b0, from, p0);
+                fetch_scale(f, na, nb, from);
             }
-    }
-    // register v of lane (r, g): row 8 (v / 4) + 4 g + v % 4, column r
+            if constexpr (decltype(more)::value) {
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
+                for (int l = q * T::kLoads / P; l < (q + 1) * T::kLoads / P; ++l) request_one(l, c + STAGES, slot);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        slot = nslot;
+        ++c;
+    };
+    while (c < steady) stage(std::true_type{});
+    do stage(std::false_type{});
+    while (c < chunks);
+    // register v of lane (r, g): row 8 (v / 4) + 4 g + v % 4, column r.  Stores go through a buffer that begins at the fragment's first row and
+    // ends with the matrix, so that rows past M fall away; columns past N get an offset past its end.
+    const float* bias_s = reinterpret_cast<const float*>(mx4_mem + STAGES * T::kStage) + wn * (32 * FN) + r;
+#pragma unroll
+    for (int j = 0; j < FN; ++j) {
         const int n = n_base + 32 * j + r;
-        const float b = n < N && bias ? bias[n] : 0.0f;
+        const float b = bias ? bias_s[32 * j] : 0.0f;
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int i = 0; i < FM; ++i) {
+            const int m = m_base + 32 * i;
+            if constexpr (ACT == ACT_SIGN) {
 #pragma unroll
-            for (int v = 0; v < 16; ++v) {
-                const int m = m_base + 32 * i + 8 * (v >> 2) + 4 * g + (v & 3);
-                const float h = acc[i][j][v] + b;
-                if constexpr (ACT == ACT_SIGN) {
-                    const unsigned long long bits = __builtin_amdgcn_ballot_w64(n < N && sign_bit(h));
-                    const int word = (n_base >> 5) + j;
-                    if (r == 0 && m < M && word < yw32) static_cast<uint32_t*>(Y)[(size_t)m * yw32 + word] = (uint32_t)(bits >> (32 * g));
-                } else {
-                    if (m < M && n < N) static_cast<float*>(Y)[(size_t)m * N + n] = mx4_act<ACT>(h);
+                for (int v = 0; v < 16; ++v) {
+                    const unsigned long long bits = __builtin_amdgcn_ballot_w64(n < N && sign_bit(acc[i][j][v] + b));
+                    const int word = (n_base >> 5) + j, mv = m + 8 * (v >> 2) + 4 * g + (v & 3);
+                    if (r == 0 && mv < M && word < yw32) static_cast<uint32_t*>(Y)[(size_t)mv * yw32 + word] = (uint32_t)(bits >> (32 * g));
                 }
+            } else {
+                const int stride = N * 4, rows = __builtin_amdgcn_readfirstlane(min(max(M - m, 0), 32));   // (32 rows of 2^22 columns: 2^29 bytes)
+                const uint64_t first = reinterpret_cast<uint64_t>(Y) + (size_t)min(m, M) * N * 4;
+                const uint64_t low = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)first), high = (uint32_t)__builtin_amdgcn_readfirstlane((int)(first >> 32));
+                const auto out = __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>(low | high << 32), 0, rows * stride, 0x00020000);
+                const int at = n < N ? 4 * g * stride + n * 4 : 0x7FFFFFFF;
+                auto store = [&](auto policy) {
+#pragma unroll
+                    for (int v = 0; v < 16; ++v)
+                        __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(mx4_act<ACT>(acc[i][j][v] + b)), out, at, (8 * (v >> 2) + (v & 3)) * stride,
+                                                              decltype(policy)::value);
+                };
+                if (nt) store(std::integral_constant<int, 2>{});   // past the caches
+                else store(std::integral_constant<int, 0>{});
             }
+        }
     }
 }
 

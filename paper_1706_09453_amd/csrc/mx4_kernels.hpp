@@ -8,6 +8,8 @@
 
 namespace bnn {
 
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+
 constexpr int kMx4Chunk = 128;        // elements of a chunk: 64 bytes of codes, one word of scale bytes
 constexpr int kMx4ChunkBytes = 64;
 __host__ __device__ inline int64_t mx4_chunks(int64_t K) { return (K + kMx4Chunk - 1) / kMx4Chunk; }
@@ -20,93 +22,162 @@ __host__ __device__ inline const uint32_t* mx4_scales(const void* q, int64_t R, 
     return reinterpret_cast<const uint32_t*>(static_cast<const unsigned char*>(q) + mx4_code_bytes(R, K));
 }
 
-// Code of a scaled number y, |y| <= 6: the 4-bit numbers 0, 0.5, 1, 1.5, 2, 3, 4, 6 are codes 0 to 7, which from 1 on are the
-// upper bits of the float (exponent and one bit of fraction, 252 = 2 * 126 above the code) and below 2 twice the value.
-// Nearest: ties to the even code.  Stochastic: the code below, or the next one up with the probability of how far y is beyond it;
-// bits16 are the random bits.  Both add to the bits that fall away and cut them off.
-__device__ __forceinline__ uint32_t mx4_code_nearest(float y) {
-    const uint32_t a = __float_as_uint(y) & 0x7FFFFFFFu;
-    const uint32_t low = (uint32_t)__builtin_rintf(2.0f * __uint_as_float(a));
-    const uint32_t high = ((a + 0x1FFFFFu + ((a >> 22) & 1u)) >> 22) - 252u;
-    return (a < 0x3F800000u ? low : high) | ((__float_as_uint(y) >> 28) & 8u);
+// Codes of 8 neighbouring numbers of a block with scale byte e, as one dword.  The 4-bit numbers 0, 0.5, 1, 1.5, 2, 3, 4, 6 are codes 0 to 7.
+// Nearest: the instruction's rounding (v_cvt_scalef32_pk_fp4_f32: ties to the even code, the scale taken from its exponent field; compared with
+// the definition on 3e7 numbers of every scale, ties and their neighbours among them).
+// Stochastic: the code below |y|, y the scaled number, or the next one up with the probability of how far |y| is beyond it.  From 1 on codes are the
+// upper bits of the float (exponent and one bit of fraction, 252 = 2 * 126 above the code), below 1 twice the value; the random bits are added to
+// the 22 that fall away.
+__device__ __forceinline__ uint32_t mx4_nearest8(const float (&v)[8], uint32_t e) {
+    const float s = __uint_as_float(e << 23);
+    uint32_t c = 0;
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[0], v[1], s, 0);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[2], v[3], s, 1);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[4], v[5], s, 2);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[6], v[7], s, 3);
+    return e == 255 ? 0u : c;
 }
 __device__ __forceinline__ uint32_t mx4_code_stochastic(float y, uint32_t bits16) {
     const uint32_t a = __float_as_uint(y) & 0x7FFFFFFFu;
     const bool small = a < 0x3F800000u;
     const uint32_t v = small ? (uint32_t)(__uint_as_float(a) * 0x1p23f) : a;
-    return ((v + (bits16 << 6)) >> 22) - (small ? 0u : 252u) | ((__float_as_uint(y) >> 28) & 8u);
+    return (((v + (bits16 << 6)) >> 22) - (small ? 0u : 252u)) | ((__float_as_uint(y) >> 28) & 8u);
+}
+// h(j): the random bits of number j, in the lower 16 bits
+template <class H>
+__device__ __forceinline__ uint32_t mx4_stochastic8(const float (&v)[8], uint32_t e, H&& h) {
+    const float inv = mx_inverse_scale(e);
+    uint32_t c = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) c |= mx4_code_stochastic(v[j] * inv, h(j) & 0xFFFFu) << (4 * j);
+    return e == 255 ? 0u : c;
+}
+__device__ __forceinline__ uint32_t mx4_top8(const float (&v)[8]) {
+    uint32_t t = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) t = max(t, __float_as_uint(v[j]) & 0x7FFFFFFFu);
+    return t;
 }
 
-// 4-bit codes of a matrix X [R][C] along its rows (Q: [R][C]) and along its columns (QT: [C][R]); either may be absent.  A workgroup
-// takes tiles of 128 x 128, for the rows form with 32 lanes per row (4 consecutive elements each, so that 8 lanes hold a block),
-// for the columns form with a column and 32 rows of it per lane.  Elements outside the matrix count as 0: pads are 0.
-template <bool VEC, bool STOCHASTIC>
-__global__ __launch_bounds__(256) void mx4_quantize_kernel(const float* __restrict__ X, int R, int C, uint32_t key, void* __restrict__ Q,
-                                                           void* __restrict__ QT, int tiles_r, int tiles_c) {
-    const int wave = (int)threadIdx.x >> 6, lane = lane_id();
+// 8 numbers of row r from column c on; 0 outside the matrix
+template <bool VEC>
+__device__ __forceinline__ void mx4_load8(const float* __restrict__ X, int R, int C, int r, int c, float (&v)[8]) {
+    const float* p = X + (size_t)r * C + c;
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+        if constexpr (VEC) {   // (C is a multiple of 4)
+            const float4 f = r < R && c + 4 * q < C ? *reinterpret_cast<const float4*>(p + 4 * q) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            v[4 * q] = f.x; v[4 * q + 1] = f.y; v[4 * q + 2] = f.z; v[4 * q + 3] = f.w;
+        } else {
+#pragma unroll
+            for (int j = 4 * q; j < 4 * q + 4; ++j) v[j] = r < R && c + j < C ? p[j] : 0.0f;
+        }
+    }
+}
+
+// A row's chunk on 16 lanes, 8 numbers each (`sub` the lane's number, four lanes a block): the lane's dword of codes, and its block's scale byte.
+template <bool STOCHASTIC>
+__device__ __forceinline__ uint32_t mx4_row_codes(const float (&v)[8], uint32_t row_key, int c, uint32_t& e) {
+    e = mx_scale<MxE2M1>(max_of_4_lanes(mx4_top8(v)));
+    if constexpr (STOCHASTIC) return mx4_stochastic8(v, e, [&](int j) { return mix32(row_key + (uint32_t)(c + j)); });
+    else return mx4_nearest8(v, e);
+}
+
+// 4-bit codes of X [R][C] along its rows, Q [R][C].  Bound by memory: a workgroup takes 16 PASSES rows of a chunk, all of it requested before
+// the first is used; consecutive workgroups go along the row.  Grid: row groups * chunks, the chunks fastest.
+template <bool VEC, bool STOCHASTIC, int PASSES>
+__global__ __launch_bounds__(256) void mx4_quantize_rows_kernel(const float* __restrict__ X, int R, int C, uint32_t key, void* __restrict__ Q, int chunks) {
+    const int64_t items = (int64_t)((R + 16 * PASSES - 1) / (16 * PASSES)) * chunks;
+    unsigned char* codes = static_cast<unsigned char*>(Q);
+    unsigned char* scales = reinterpret_cast<unsigned char*>(mx4_scales(Q, R, C));
+    const int sub = (int)threadIdx.x & 15;
+    for (int64_t i = blockIdx.x; i < items; i += gridDim.x) {
+        const int64_t group = i / chunks;
+        const int chunk = (int)(i - group * chunks), r0 = (int)group * (16 * PASSES) + ((int)threadIdx.x >> 4), c = chunk * kMx4Chunk + 8 * sub;
+        float v[PASSES][8];
+#pragma unroll
+        for (int p = 0; p < PASSES; ++p) mx4_load8<VEC>(X, R, C, r0 + 16 * p, c, v[p]);
+#pragma unroll
+        for (int p = 0; p < PASSES; ++p) {
+            const int r = r0 + 16 * p;
+            uint32_t e;
+            const uint32_t w = mx4_row_codes<STOCHASTIC>(v[p], STOCHASTIC ? mix32(key + (uint32_t)r) : 0u, c, e);
+            if (r < R) {
+                *reinterpret_cast<uint32_t*>(codes + ((size_t)r * chunks + chunk) * kMx4ChunkBytes + 4 * sub) = w;
+                if ((sub & 3) == 0) scales[((size_t)chunk * R + r) * 4 + (sub >> 2)] = (unsigned char)e;
+            }
+        }
+    }
+}
+
+// Along its columns, QT [C][R], and with ROWS along its rows too, from one read.  A workgroup takes 128 x 128 numbers, a chunk of both
+// forms.  A lane holds 32 rows of a column, a block of the columns form, twice; for the rows form the wave's 32 rows go through LDS.  What the
+// columns form writes is collected in LDS, so that it leaves as 64 bytes per column and whole lines of scale words.
+constexpr int kMx4TileLd = 128 + 4;   // floats of a row in LDS
+template <bool STOCHASTIC, bool ROWS>
+__global__ __launch_bounds__(256) void mx4_quantize_columns_kernel(const float* __restrict__ X, int R, int C, uint32_t key, void* __restrict__ Q,
+                                                                   void* __restrict__ QT, int tiles_r, int tiles_c) {
+    __shared__ __attribute__((aligned(16))) float rows_s[ROWS ? 4 : 1][ROWS ? 32 : 1][kMx4TileLd];
+    __shared__ __attribute__((aligned(16))) uint4 codes_s[128][4];
+    __shared__ unsigned char scales_s[2][128][4];   // columns, rows
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = lane_id();
+    unsigned char *codes_q = static_cast<unsigned char*>(Q), *codes_t = static_cast<unsigned char*>(QT);
+    uint32_t *scales_q = ROWS ? mx4_scales(Q, R, C) : nullptr, *scales_t = mx4_scales(QT, C, R);
     for (int64_t t = blockIdx.x; t < (int64_t)tiles_r * tiles_c; t += gridDim.x) {
-        const int tc = (int)(t % tiles_c), tr = (int)(t / tiles_c), c0 = tc * 128, r0 = tr * 128;
-        if (Q) {
-            unsigned char* codes = static_cast<unsigned char*>(Q);
-            unsigned char* scales = reinterpret_cast<unsigned char*>(mx4_scales(Q, R, C));
-            const int sub = lane & 31, c = c0 + 4 * sub;
-            for (int i = 0; i < 16; ++i) {
-                const int r = r0 + 8 * i + 2 * wave + (lane >> 5);
-                if (r >= R) continue;   // (whole groups of 32 lanes)
-                float v[4];
-                const float* p = X + (size_t)r * C + c;
-                if (VEC && c + 4 <= C) {
-                    const float4 q = *reinterpret_cast<const float4*>(p);
-                    v[0] = q.x; v[1] = q.y; v[2] = q.z; v[3] = q.w;
-                } else {
+        const int tr = (int)(t / tiles_c), tc = (int)(t - (int64_t)tr * tiles_c), c0 = tc * 128, r0 = tr * 128, rb = r0 + 32 * wave;
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) v[j] = c + j < C ? p[j] : 0.0f;
-                }
-                uint32_t top = 0;
+        for (int h = 0; h < 2; ++h) {
+            const int cl = 64 * h + lane, c = c0 + cl;
+            float v[32];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) top = max(top, __float_as_uint(v[j]) & 0x7FFFFFFFu);
-                top = max_of_8_lanes(top);
-                const uint32_t e = mx_scale<MxE2M1>(top);
-                const float inv = mx_inverse_scale(e);
-                const uint32_t row_key = mix32(key + (uint32_t)r);
-                uint32_t out = 0;
+            for (int j = 0; j < 32; ++j) v[j] = rb + j < R && c < C ? X[(size_t)(rb + j) * C + c] : 0.0f;
+            uint32_t top = 0;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const float y = v[j] * inv;
-                    const uint32_t code = STOCHASTIC ? mx4_code_stochastic(y, mix32(row_key + (uint32_t)(c + j)) & 0xFFFFu) : mx4_code_nearest(y);
-                    out |= code << (4 * j);
-                }
-                if (e == 255) out = 0;
-                *reinterpret_cast<uint16_t*>(codes + ((size_t)r * tiles_c + tc) * 64 + 2 * sub) = (uint16_t)out;
-                if ((sub & 7) == 0) scales[((size_t)tc * R + r) * 4 + (sub >> 3)] = (unsigned char)e;
+            for (int j = 0; j < 32; ++j) top = max(top, __float_as_uint(v[j]) & 0x7FFFFFFFu);
+            const uint32_t e = mx_scale<MxE2M1>(top);
+            uint32_t w[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const float x[8] = {v[8 * q], v[8 * q + 1], v[8 * q + 2], v[8 * q + 3], v[8 * q + 4], v[8 * q + 5], v[8 * q + 6], v[8 * q + 7]};
+                if constexpr (STOCHASTIC) w[q] = mx4_stochastic8(x, e, [&](int j) { return mix32(mix32(key + (uint32_t)(rb + 8 * q + j)) + (uint32_t)c) >> 16; });
+                else w[q] = mx4_nearest8(x, e);
+            }
+            codes_s[cl][wave] = make_uint4(w[0], w[1], w[2], w[3]);
+            scales_s[0][cl][wave] = (unsigned char)e;
+            if constexpr (ROWS) {
+#pragma unroll
+                for (int j = 0; j < 32; ++j) rows_s[wave][j][cl] = v[j];
             }
         }
-        if (QT) {
-            unsigned char* codes = static_cast<unsigned char*>(QT);
-            unsigned char* scales = reinterpret_cast<unsigned char*>(mx4_scales(QT, C, R));
-            for (int h = 0; h < 2; ++h) {
-                const int c = c0 + 64 * h + lane, rb = r0 + 32 * wave;
-                if (c >= C) continue;
-                float v[32];
-                uint32_t top = 0;
+        if constexpr (ROWS) {   // (a wave reads what it wrote itself)
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");
+            const int sub = lane & 15, c = c0 + 8 * sub;
 #pragma unroll
-                for (int j = 0; j < 32; ++j) v[j] = rb + j < R ? X[(size_t)(rb + j) * C + c] : 0.0f;
-#pragma unroll
-                for (int j = 0; j < 32; ++j) top = max(top, __float_as_uint(v[j]) & 0x7FFFFFFFu);
-                const uint32_t e = mx_scale<MxE2M1>(top);
-                const float inv = mx_inverse_scale(e);
-                uint32_t w[4] = {0u, 0u, 0u, 0u};
-#pragma unroll
-                for (int j = 0; j < 32; ++j) {
-                    const float y = v[j] * inv;
-                    const uint32_t code = STOCHASTIC ? mx4_code_stochastic(y, mix32(mix32(key + (uint32_t)(rb + j)) + (uint32_t)c) >> 16) : mx4_code_nearest(y);
-                    w[j >> 3] |= code << (4 * (j & 7));
-                }
-                if (e == 255) w[0] = w[1] = w[2] = w[3] = 0u;
-                *reinterpret_cast<uint4*>(codes + ((size_t)c * tiles_r + tr) * 64 + 16 * wave) = make_uint4(w[0], w[1], w[2], w[3]);
-                scales[((size_t)tr * C + c) * 4 + wave] = (unsigned char)e;
+            for (int i = 0; i < 8; ++i) {
+                const int j = 4 * i + (lane >> 4), r = rb + j;
+                const float4 lo = *reinterpret_cast<const float4*>(&rows_s[wave][j][8 * sub]), hi = *reinterpret_cast<const float4*>(&rows_s[wave][j][8 * sub + 4]);
+                const float x[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+                uint32_t e;
+                const uint32_t w = mx4_row_codes<STOCHASTIC>(x, STOCHASTIC ? mix32(key + (uint32_t)r) : 0u, c, e);
+                if (r < R) *reinterpret_cast<uint32_t*>(codes_q + ((size_t)r * tiles_c + tc) * kMx4ChunkBytes + 4 * sub) = w;
+                if ((sub & 3) == 0) scales_s[1][32 * wave + j][sub >> 2] = (unsigned char)e;
             }
         }
+        __syncthreads();
+        {
+            const int n = (int)threadIdx.x;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int cl = (n >> 2) + 64 * i;
+                if (c0 + cl < C) *reinterpret_cast<uint4*>(codes_t + ((size_t)(c0 + cl) * tiles_r + tr) * kMx4ChunkBytes + 16 * (n & 3)) = codes_s[cl][n & 3];
+            }
+            if (n < 128) {
+                if (c0 + n < C) scales_t[(size_t)tr * C + c0 + n] = *reinterpret_cast<const uint32_t*>(scales_s[0][n]);
+            } else if (ROWS) {
+                if (r0 + n - 128 < R) scales_q[(size_t)tc * R + r0 + n - 128] = *reinterpret_cast<const uint32_t*>(scales_s[1][n - 128]);
+            }
+        }
+        __syncthreads();   // (before the next tile)
     }
 }
 
@@ -121,13 +192,9 @@ __global__ __launch_bounds__(256) void mx4_dequantize_kernel(const void* __restr
         const int r = (int)(rc / chunks), chunk = (int)(rc - (int64_t)r * chunks), sub = (int)(i & 31), k = chunk * 128 + 4 * sub;
         if (k >= K) continue;
         const uint32_t c = *reinterpret_cast<const uint16_t*>(codes + 2 * i);
-        const float s = mx_scale_value(scales[((size_t)chunk * R + r) * 4 + (sub >> 3)]);
-        float v[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const uint32_t n = c >> (4 * j);   // the code's lower bits are a float's exponent and fraction, 2^126 too small
-            v[j] = __uint_as_float((n & 7u) << 22 | (n & 8u) << 28) * 0x1p126f * s;
-        }
+        const float s = __uint_as_float((uint32_t)scales[((size_t)chunk * R + r) * 4 + (sub >> 3)] << 23);   // (the instruction takes the field: 0 is 2^-127, 255 NaN)
+        const f32x2 lo = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, s, 0), hi = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, s, 1);
+        const float v[4] = {lo.x, lo.y, hi.x, hi.y};
         float* p = X + (size_t)r * K + k;
         if (VEC && k + 4 <= K) {
             *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);

@@ -37,16 +37,13 @@ __device__ __forceinline__ float mx_scale_value(uint32_t e) { return __uint_as_f
 // 2^(127 - e) for a scale byte from mx_scale; 0 for 255, which with finite numbers gives codes of 0 (the caller keeps Inf and NaN out)
 __device__ __forceinline__ float mx_inverse_scale(uint32_t e) { return __uint_as_float(e == 255 ? 0u : (254u - e) << 23); }
 
-// the largest of 8 neighbouring lanes' values, in all of them
-__device__ __forceinline__ uint32_t max_of_8_lanes(uint32_t v) {
-    auto take = [&](auto ctrl) {
-        const uint32_t o = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, decltype(ctrl)::value, 0xF, 0xF, false);
-        v = o > v ? o : v;
-    };
-    take(std::integral_constant<int, 0xB1>{});    // quad_perm [1, 0, 3, 2]
-    take(std::integral_constant<int, 0x4E>{});    // quad_perm [2, 3, 0, 1]
-    take(std::integral_constant<int, 0x141>{});   // row_half_mirror: lane i and 7 - i of every 8
-    return v;
+// the larger of the lane's value and another lane's (CTRL: a DPP control)
+template <int CTRL>
+__device__ __forceinline__ uint32_t max_dpp(uint32_t v) {
+    return max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xF, 0xF, false));
 }
+// the largest of 4 and of 8 neighbouring lanes' values, in all of them
+__device__ __forceinline__ uint32_t max_of_4_lanes(uint32_t v) { return max_dpp<0x4E>(max_dpp<0xB1>(v)); }   // quad_perm [1, 0, 3, 2], [2, 3, 0, 1]
+__device__ __forceinline__ uint32_t max_of_8_lanes(uint32_t v) { return max_dpp<0x141>(max_of_4_lanes(v)); }   // row_half_mirror: lane i and 7 - i of every 8
 
 }  // namespace bnn
