@@ -19,18 +19,18 @@ bool mx4_dims_ok(int64_t R, int64_t K) { return R > 0 && K > 0 && R <= kMaxDim &
 
 template <bool VEC, bool STOCHASTIC>
 void launch_quantize(const float* X, int R, int C, uint32_t key, void* Q, void* QT, hipStream_t st) {
-    const int tr = (R + 127) / 128, tc = (C + 127) / 128;
     auto grid = [](int64_t n) { return dim3((unsigned)(n < 65536 ? n : 65536)); };
+    const int chunks = (C + 127) / 128, tr = (R + 127) / 128, tc = (C + 63) / 64;
     if (!QT) {
         // 16 rows a workgroup while that leaves CUs idle, 32 beyond
-        if ((int64_t)((R + 31) / 32) * tc < 512)
-            mx4_quantize_rows_kernel<VEC, STOCHASTIC, 1><<<grid((int64_t)((R + 15) / 16) * tc), 256, 0, st>>>(X, R, C, key, Q, tc);
+        if ((int64_t)((R + 31) / 32) * chunks < 512)
+            mx4_quantize_rows_kernel<VEC, STOCHASTIC, 1><<<grid((int64_t)((R + 15) / 16) * chunks), 256, 0, st>>>(X, R, C, key, Q, chunks);
         else
-            mx4_quantize_rows_kernel<VEC, STOCHASTIC, 2><<<grid((int64_t)((R + 31) / 32) * tc), 256, 0, st>>>(X, R, C, key, Q, tc);
+            mx4_quantize_rows_kernel<VEC, STOCHASTIC, 2><<<grid((int64_t)((R + 31) / 32) * chunks), 256, 0, st>>>(X, R, C, key, Q, chunks);
     } else if (!Q) {
-        mx4_quantize_columns_kernel<STOCHASTIC, false><<<grid((int64_t)tr * tc), 256, 0, st>>>(X, R, C, key, Q, QT, tr, tc);
+        mx4_quantize_columns_kernel<STOCHASTIC, false><<<grid(((int64_t)tr * tc + 7) / 8 * 8), 256, 0, st>>>(X, R, C, key, Q, QT, tr, tc);
     } else {
-        mx4_quantize_columns_kernel<STOCHASTIC, true><<<grid((int64_t)tr * tc), 256, 0, st>>>(X, R, C, key, Q, QT, tr, tc);
+        mx4_quantize_columns_kernel<STOCHASTIC, true><<<grid(((int64_t)tr * tc + 7) / 8 * 8), 256, 0, st>>>(X, R, C, key, Q, QT, tr, tc);
     }
 }
 int run_quantize(const float* X, int64_t R, int64_t C, int rounding, uint64_t seed, void* Q, void* QT, hipStream_t st) {

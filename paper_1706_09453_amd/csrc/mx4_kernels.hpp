@@ -25,9 +25,10 @@ __host__ __device__ inline const uint32_t* mx4_scales(const void* q, int64_t R, 
 // Codes of 8 neighbouring numbers of a block with scale byte e, as one dword.  The 4-bit numbers 0, 0.5, 1, 1.5, 2, 3, 4, 6 are codes 0 to 7.
 // Nearest: the instruction's rounding (v_cvt_scalef32_pk_fp4_f32: ties to the even code, the scale taken from its exponent field; compared with
 // the definition on 3e7 numbers of every scale, ties and their neighbours among them).
-// Stochastic: the code below |y|, y the scaled number, or the next one up with the probability of how far |y| is beyond it.  From 1 on codes are the
-// upper bits of the float (exponent and one bit of fraction, 252 = 2 * 126 above the code), below 1 twice the value; the random bits are added to
-// the 22 that fall away.
+// Stochastic: the code below, or the next one up with the probability of how far the number is beyond it (v_cvt_scalef32_sr_pk_fp4_f32: of the
+// upper 16 of the seed's bits as a fraction of the gap, the lower ones 0, their sum with the number cut off.  The instruction's second number takes
+// the seed from bit 30 down; numbers that have bits of their own go one by one, beside a 0, which stays one).  Compared with the definition on
+// 5e8 numbers likewise.
 __device__ __forceinline__ uint32_t mx4_nearest8(const float (&v)[8], uint32_t e) {
     const float s = __uint_as_float(e << 23);
     uint32_t c = 0;
@@ -37,20 +38,17 @@ __device__ __forceinline__ uint32_t mx4_nearest8(const float (&v)[8], uint32_t e
     c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[6], v[7], s, 3);
     return e == 255 ? 0u : c;
 }
-__device__ __forceinline__ uint32_t mx4_code_stochastic(float y, uint32_t bits16) {
-    const uint32_t a = __float_as_uint(y) & 0x7FFFFFFFu;
-    const bool small = a < 0x3F800000u;
-    const uint32_t v = small ? (uint32_t)(__uint_as_float(a) * 0x1p23f) : a;
-    return (((v + (bits16 << 6)) >> 22) - (small ? 0u : 252u)) | ((__float_as_uint(y) >> 28) & 8u);
-}
-// h(j): the random bits of number j, in the lower 16 bits
+// h(j): the 16 random bits of number j
 template <class H>
 __device__ __forceinline__ uint32_t mx4_stochastic8(const float (&v)[8], uint32_t e, H&& h) {
-    const float inv = mx_inverse_scale(e);
-    uint32_t c = 0;
+    const float s = __uint_as_float(e << 23);
+    uint32_t pair[4];   // (in the lowest byte; the others are not to be relied on)
 #pragma unroll
-    for (int j = 0; j < 8; ++j) c |= mx4_code_stochastic(v[j] * inv, h(j) & 0xFFFFu) << (4 * j);
-    return e == 255 ? 0u : c;
+    for (int j = 0; j < 4; ++j)
+        pair[j] = __builtin_amdgcn_cvt_scalef32_sr_pk_fp4_f32(0u, f32x2{v[2 * j], 0.0f}, h(2 * j) << 16, s, 0) |
+                  __builtin_amdgcn_cvt_scalef32_sr_pk_fp4_f32(0u, f32x2{0.0f, v[2 * j + 1]}, h(2 * j + 1) << 15, s, 0);
+    const uint32_t low = __builtin_amdgcn_perm(pair[1], pair[0], 0x0C0C0400u), high = __builtin_amdgcn_perm(pair[3], pair[2], 0x04000C0Cu);
+    return e == 255 ? 0u : low | high;
 }
 __device__ __forceinline__ uint32_t mx4_top8(const float (&v)[8]) {
     uint32_t t = 0;
@@ -75,14 +73,6 @@ __device__ __forceinline__ void mx4_load8(const float* __restrict__ X, int R, in
     }
 }
 
-// A row's chunk on 16 lanes, 8 numbers each (`sub` the lane's number, four lanes a block): the lane's dword of codes, and its block's scale byte.
-template <bool STOCHASTIC>
-__device__ __forceinline__ uint32_t mx4_row_codes(const float (&v)[8], uint32_t row_key, int c, uint32_t& e) {
-    e = mx_scale<MxE2M1>(max_of_4_lanes(mx4_top8(v)));
-    if constexpr (STOCHASTIC) return mx4_stochastic8(v, e, [&](int j) { return mix32(row_key + (uint32_t)(c + j)); });
-    else return mx4_nearest8(v, e);
-}
-
 // 4-bit codes of X [R][C] along its rows, Q [R][C].  Bound by memory: a workgroup takes 16 PASSES rows of a chunk, all of it requested before
 // the first is used; consecutive workgroups go along the row.  Grid: row groups * chunks, the chunks fastest.
 template <bool VEC, bool STOCHASTIC, int PASSES>
@@ -100,8 +90,14 @@ __global__ __launch_bounds__(256) void mx4_quantize_rows_kernel(const float* __r
 #pragma unroll
         for (int p = 0; p < PASSES; ++p) {
             const int r = r0 + 16 * p;
-            uint32_t e;
-            const uint32_t w = mx4_row_codes<STOCHASTIC>(v[p], STOCHASTIC ? mix32(key + (uint32_t)r) : 0u, c, e);
+            const uint32_t e = mx_scale<MxE2M1>(max_of_4_lanes(mx4_top8(v[p])));   // (four lanes a block)
+            uint32_t w;
+            if constexpr (STOCHASTIC) {
+                const uint32_t row_key = mix32(key + (uint32_t)r);
+                w = mx4_stochastic8(v[p], e, [&](int j) { return mix32(row_key + (uint32_t)(c + j)) & 0xFFFFu; });
+            } else {
+                w = mx4_nearest8(v[p], e);
+            }
             if (r < R) {
                 *reinterpret_cast<uint32_t*>(codes + ((size_t)r * chunks + chunk) * kMx4ChunkBytes + 4 * sub) = w;
                 if ((sub & 3) == 0) scales[((size_t)chunk * R + r) * 4 + (sub >> 2)] = (unsigned char)e;
@@ -110,27 +106,38 @@ __global__ __launch_bounds__(256) void mx4_quantize_rows_kernel(const float* __r
     }
 }
 
-// Along its columns, QT [C][R], and with ROWS along its rows too, from one read.  A workgroup takes 128 x 128 numbers, a chunk of both
-// forms.  A lane holds 32 rows of a column, a block of the columns form, twice; for the rows form the wave's 32 rows go through LDS.  What the
-// columns form writes is collected in LDS, so that it leaves as 64 bytes per column and whole lines of scale words.
-constexpr int kMx4TileLd = 128 + 4;   // floats of a row in LDS
+// Along its columns, QT [C][R], and with ROWS along its rows too.  A workgroup takes 128 rows (a chunk of the columns form) of 64 columns.  For the
+// columns form a lane holds 32 rows of a column, a block; what it writes is collected in LDS, so that it leaves as 64 bytes per column and whole
+// lines of scale words.  For the rows form the wave's numbers go through LDS: 8 lanes a row, 8 numbers each.  (Their random bits are mixed once
+// more: handed on through LDS as well, they cost more in workgroups per CU than they save, 16384 x 4096 120 us against 96.)
+// Workgroups go round the eight XCDs: each takes a run of consecutive tiles, so that the pieces of a line that several of them write meet in one
+// L2.  Grid: a multiple of 8.
+constexpr int kMx4TileLd = 64 + 4;   // floats of a row in LDS
 template <bool STOCHASTIC, bool ROWS>
 __global__ __launch_bounds__(256) void mx4_quantize_columns_kernel(const float* __restrict__ X, int R, int C, uint32_t key, void* __restrict__ Q,
                                                                    void* __restrict__ QT, int tiles_r, int tiles_c) {
     __shared__ __attribute__((aligned(16))) float rows_s[ROWS ? 4 : 1][ROWS ? 32 : 1][kMx4TileLd];
-    __shared__ __attribute__((aligned(16))) uint4 codes_s[128][4];
-    __shared__ unsigned char scales_s[2][128][4];   // columns, rows
+    __shared__ __attribute__((aligned(16))) uint4 codes_s[64][4];
+    __shared__ __attribute__((aligned(4))) unsigned char scales_s[64][4];
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = lane_id();
     unsigned char *codes_q = static_cast<unsigned char*>(Q), *codes_t = static_cast<unsigned char*>(QT);
-    uint32_t *scales_q = ROWS ? mx4_scales(Q, R, C) : nullptr, *scales_t = mx4_scales(QT, C, R);
-    for (int64_t t = blockIdx.x; t < (int64_t)tiles_r * tiles_c; t += gridDim.x) {
-        const int tr = (int)(t / tiles_c), tc = (int)(t - (int64_t)tr * tiles_c), c0 = tc * 128, r0 = tr * 128, rb = r0 + 32 * wave;
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int cl = 64 * h + lane, c = c0 + cl;
+    unsigned char* scales_q = ROWS ? reinterpret_cast<unsigned char*>(mx4_scales(Q, R, C)) : nullptr;
+    uint32_t* scales_t = mx4_scales(QT, C, R);
+    const int chunks_q = (C + 127) / 128;
+    const int64_t total = (int64_t)tiles_r * tiles_c, per_xcd = (total + 7) >> 3;
+    for (int64_t k = blockIdx.x >> 3; k < per_xcd; k += gridDim.x >> 3) {
+        const int64_t t = (blockIdx.x & 7) * per_xcd + k;
+        if (t >= total) break;
+        const int tr = (int)(t / tiles_c), tc = (int)(t - (int64_t)tr * tiles_c), c0 = tc * 64, r0 = tr * 128, rb = r0 + 32 * wave;
+        {
+            const int c = c0 + lane;
             float v[32];
 #pragma unroll
             for (int j = 0; j < 32; ++j) v[j] = rb + j < R && c < C ? X[(size_t)(rb + j) * C + c] : 0.0f;
+            if constexpr (ROWS) {
+#pragma unroll
+                for (int j = 0; j < 32; ++j) rows_s[wave][j][lane] = v[j];
+            }
             uint32_t top = 0;
 #pragma unroll
             for (int j = 0; j < 32; ++j) top = max(top, __float_as_uint(v[j]) & 0x7FFFFFFFu);
@@ -139,42 +146,44 @@ __global__ __launch_bounds__(256) void mx4_quantize_columns_kernel(const float* 
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 const float x[8] = {v[8 * q], v[8 * q + 1], v[8 * q + 2], v[8 * q + 3], v[8 * q + 4], v[8 * q + 5], v[8 * q + 6], v[8 * q + 7]};
-                if constexpr (STOCHASTIC) w[q] = mx4_stochastic8(x, e, [&](int j) { return mix32(mix32(key + (uint32_t)(rb + 8 * q + j)) + (uint32_t)c) >> 16; });
+                if constexpr (STOCHASTIC)
+                    w[q] = mx4_stochastic8(x, e, [&](int j) { return mix32(mix32(key + (uint32_t)(rb + 8 * q + j)) + (uint32_t)c) >> 16; });
                 else w[q] = mx4_nearest8(x, e);
             }
-            codes_s[cl][wave] = make_uint4(w[0], w[1], w[2], w[3]);
-            scales_s[0][cl][wave] = (unsigned char)e;
-            if constexpr (ROWS) {
-#pragma unroll
-                for (int j = 0; j < 32; ++j) rows_s[wave][j][cl] = v[j];
-            }
-        }
-        if constexpr (ROWS) {   // (a wave reads what it wrote itself)
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");
-            const int sub = lane & 15, c = c0 + 8 * sub;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int j = 4 * i + (lane >> 4), r = rb + j;
-                const float4 lo = *reinterpret_cast<const float4*>(&rows_s[wave][j][8 * sub]), hi = *reinterpret_cast<const float4*>(&rows_s[wave][j][8 * sub + 4]);
-                const float x[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
-                uint32_t e;
-                const uint32_t w = mx4_row_codes<STOCHASTIC>(x, STOCHASTIC ? mix32(key + (uint32_t)r) : 0u, c, e);
-                if (r < R) *reinterpret_cast<uint32_t*>(codes_q + ((size_t)r * tiles_c + tc) * kMx4ChunkBytes + 4 * sub) = w;
-                if ((sub & 3) == 0) scales_s[1][32 * wave + j][sub >> 2] = (unsigned char)e;
-            }
+            codes_s[lane][wave] = make_uint4(w[0], w[1], w[2], w[3]);
+            scales_s[lane][wave] = (unsigned char)e;
         }
         __syncthreads();
         {
-            const int n = (int)threadIdx.x;
+            const int n = (int)threadIdx.x, c = c0 + (n >> 2);
+            if (c < C) *reinterpret_cast<uint4*>(codes_t + ((size_t)c * tiles_r + tr) * kMx4ChunkBytes + 16 * (n & 3)) = codes_s[n >> 2][n & 3];
+            if (n < 64 && c0 + n < C) scales_t[(size_t)tr * C + c0 + n] = *reinterpret_cast<const uint32_t*>(scales_s[n]);
+        }
+        if constexpr (ROWS) {
+            const int sub = lane & 7, piece = tc & 1;
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const int cl = (n >> 2) + 64 * i;
-                if (c0 + cl < C) *reinterpret_cast<uint4*>(codes_t + ((size_t)(c0 + cl) * tiles_r + tr) * kMx4ChunkBytes + 16 * (n & 3)) = codes_s[cl][n & 3];
-            }
-            if (n < 128) {
-                if (c0 + n < C) scales_t[(size_t)tr * C + c0 + n] = *reinterpret_cast<const uint32_t*>(scales_s[0][n]);
-            } else if (ROWS) {
-                if (r0 + n - 128 < R) scales_q[(size_t)tc * R + r0 + n - 128] = *reinterpret_cast<const uint32_t*>(scales_s[1][n - 128]);
+            for (int i = 0; i < 4; ++i) {
+                const int j = 8 * i + (lane >> 3), r = rb + j;
+                const float4 lo = *reinterpret_cast<const float4*>(&rows_s[wave][j][8 * sub]), hi = *reinterpret_cast<const float4*>(&rows_s[wave][j][8 * sub + 4]);
+                const float v[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+                const uint32_t e = mx_scale<MxE2M1>(max_of_4_lanes(mx4_top8(v)));
+                uint32_t w;
+                if constexpr (STOCHASTIC) {
+                    const uint32_t row_key = mix32(key + (uint32_t)r);
+                    w = mx4_stochastic8(v, e, [&](int n) { return mix32(row_key + (uint32_t)(c0 + 8 * sub + n)) & 0xFFFFu; });
+                } else {
+                    w = mx4_nearest8(v, e);
+                }
+                if (r < R) {
+                    const size_t chunk = (size_t)r * chunks_q + (tc >> 1);
+                    *reinterpret_cast<uint32_t*>(codes_q + chunk * kMx4ChunkBytes + 32 * piece + 4 * sub) = w;
+                    unsigned char* s = scales_q + ((size_t)(tc >> 1) * R + r) * 4 + 2 * piece;
+                    if ((sub & 3) == 0) s[sub >> 2] = (unsigned char)e;
+                    if (tc == tiles_c - 1 && !piece) {   // the chunk's other half is pad, which no workgroup has
+                        *reinterpret_cast<uint32_t*>(codes_q + chunk * kMx4ChunkBytes + 32 + 4 * sub) = 0u;
+                        if ((sub & 3) == 0) s[2 + (sub >> 2)] = 0;
+                    }
+                }
             }
         }
         __syncthreads();   // (before the next tile)
