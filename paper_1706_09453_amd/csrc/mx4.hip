@@ -56,6 +56,46 @@ bool launch_gemm(const void* Xq, const void* Wq, const float* bias, int M, int K
     return true;
 }
 
+// f with the activation that the product's kernel applies, as a constant
+template <class F>
+void with_act(int act, F&& f) {
+    switch (act) {
+        case BNN_ACT_SIGN: f(std::integral_constant<int, ACT_SIGN>{}); break;
+        case BNN_ACT_HARDTANH: f(std::integral_constant<int, ACT_HARDTANH>{}); break;
+        case BNN_ACT_SIGMOID: f(std::integral_constant<int, ACT_SIGMOID>{}); break;
+        default: f(std::integral_constant<int, ACT_LINEAR>{}); break;
+    }
+}
+
+// Up to 16 frames, and up to 64 of more than 1024 inputs: the kernel that splits K over the waves of a workgroup (16 x 2048 x 2048 3.6 us, 5.0 on tiles of
+// 64 x 64; 64 x 4096 x 4096 8.4 and 8.4, 32 x 2048 x 2048 4.1 and 5.0, but 32 x 1024 x 3400 4.4 and 4.0, 32 x 440 x 1024 4.0 and 3.2).
+bool few_frames(int64_t M, int64_t K) { return M <= 16 || (M <= 64 && K > 1024); }
+// Frames that this kernel rounds to 4 bits by itself: every workgroup rounds all of them, so few numbers only (us for it, and for the two launches without
+// the gap between them: 1 x 2048 x 2048 4.7 and 5.5, 4 x 2048 x 2048 5.3 and 5.7, 16 x 440 x 1024 5.3 and 5.5; 16 x 1024 x 3400 8.5 and 6.1).
+bool rounds_frames(int64_t M, int64_t K) { return M <= 16 && M * K <= 8192; }
+// REALX: X is fp32; vec: its rows are 16-byte aligned
+template <bool REALX>
+void go_few(const void* X, const void* Wq, const float* bias, int64_t M, int64_t K, int64_t N, int act, void* Y, int yw32, bool vec, hipStream_t st) {
+    const unsigned gx = act == BNN_ACT_SIGN ? 2u * (unsigned)yw32 : (unsigned)((N + 15) / 16);
+    auto go = [&](auto frags, auto v) {
+        constexpr int F = decltype(frags)::value;
+        constexpr bool V = decltype(v)::value;
+        with_act(act, [&](auto a) {
+            mx4_few_kernel<F, REALX, V, decltype(a)::value><<<dim3(gx, (unsigned)((M + 16 * F - 1) / (16 * F))), 256, 0, st>>>(
+                X, Wq, bias, (int)M, (int)K, (int)N, (int)mx4_chunks(K), Y, yw32);
+        });
+    };
+    using I1 = std::integral_constant<int, 1>;
+    if constexpr (REALX) {
+        if (vec) go(I1{}, std::true_type{});
+        else go(I1{}, std::false_type{});
+    } else {
+        if (M <= 16) go(I1{}, std::true_type{});
+        else if (M <= 32) go(std::integral_constant<int, 2>{}, std::true_type{});
+        else go(std::integral_constant<int, 4>{}, std::true_type{});
+    }
+}
+
 int run_layer(const void* Xq, const void* Wq, const float* bias, int64_t M, int64_t K, int64_t N, int act, int wb, void* Y, hipStream_t st) {
     const int yw32 = (int)row_w32(N, wb);
     const auto tiles = [&](int rows, int cols) { return ((M + rows - 1) / rows) * ((N + cols - 1) / cols); };
@@ -71,12 +111,8 @@ int run_layer(const void* Xq, const void* Wq, const float* bias, int64_t M, int6
         else if (tiles(256, 128) <= 512) ok = launch_gemm<4, 2, 2, 2, 3, A>(Xq, Wq, bias, (int)M, (int)K, (int)N, Y, yw32, nt, st);
         else ok = launch_gemm<4, 2, 2, 4, 4, A>(Xq, Wq, bias, (int)M, (int)K, (int)N, Y, yw32, nt, st);
     };
-    switch (act) {
-        case BNN_ACT_SIGN: go(std::integral_constant<int, ACT_SIGN>{}); break;
-        case BNN_ACT_HARDTANH: go(std::integral_constant<int, ACT_HARDTANH>{}); break;
-        case BNN_ACT_SIGMOID: go(std::integral_constant<int, ACT_SIGMOID>{}); break;
-        default: go(std::integral_constant<int, ACT_LINEAR>{}); break;
-    }
+    if (few_frames(M, K)) go_few<false>(Xq, Wq, bias, M, K, N, act, Y, yw32, false, st);
+    else with_act(act, go);
     if (!ok) return BNN_EDEVICE;
     if (act == BNN_ACT_LOGSOFTMAX) launch_log_softmax(static_cast<float*>(Y), (int)M, (int)N, st);
     return launch_status();
@@ -150,6 +186,11 @@ BNN_EXPORT int bnn_layer_mx4_realx(const float* X, const void* Wq, const float* 
         (bias && overlap(workspace, need, bias, (size_t)N * 4)))
         return BNN_EINVAL;
     hipStream_t st = static_cast<hipStream_t>(stream);
+    if (rounds_frames(M, K)) {
+        go_few<true>(X, Wq, bias, M, K, N, act, Y, (int)row_w32(N, word_bits), K % 4 == 0 && aligned(X, 16), st);
+        if (act == BNN_ACT_LOGSOFTMAX) launch_log_softmax(static_cast<float*>(Y), (int)M, (int)N, st);
+        return launch_status();
+    }
     const int q = run_quantize(X, M, K, BNN_ROUND_NEAREST, 0, workspace, nullptr, st);
     return q != BNN_OK ? q : run_layer(workspace, Wq, bias, M, K, N, act, word_bits, Y, st);
 }

@@ -218,4 +218,98 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, FM * FN > 8 ? 1 : 2) void m
     }
 }
 
+// ---- Few frames, on V_MFMA_SCALE_F32_16X16X128_F8F6F4: weights as the first operand, lane (r = lane % 16, q = lane / 16) holds block q of the
+// chunk's four of row r and its scale byte.  A workgroup takes 16 outputs of up to 16 FRAMES frames, its four waves every fourth chunk of K, all of
+// them straight from memory: what counts is how soon all of the weights are requested.  The waves' sums are joined in LDS, in order.
+// REALX: X is fp32, and a lane rounds the block that it holds to 4 bits by itself (rows of a multiple of 4 numbers, 16-byte aligned, with VEC).
+// FRAGS: fragments of 16 frames.  Grid: x = 16 outputs each (SIGN: up to the end of the row's last word), y = 16 FRAGS frames each.
+constexpr int kMx4FewAhead = 4;   // chunks that a wave requests before it uses the first
+template <int FRAGS, bool REALX, bool VEC, int ACT>
+__global__ __launch_bounds__(256) void mx4_few_kernel(const void* __restrict__ X, const void* __restrict__ Wq, const float* __restrict__ bias, int M, int K,
+                                                      int N, int chunks, void* __restrict__ Y, int yw32) {
+    static_assert(FRAGS <= 4, "a wave finishes a fragment");
+    typedef float v4f __attribute__((ext_vector_type(4)));
+    __shared__ __attribute__((aligned(16))) v4f part[4][FRAGS][64];
+    const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = lane_id(), r = lane & 15, q = lane >> 4;
+    const int n0 = (int)blockIdx.x * 16, m0 = (int)blockIdx.y * (16 * FRAGS), nr = min(n0 + r, N - 1);
+    const unsigned char* wrow = static_cast<const unsigned char*>(Wq) + (size_t)nr * chunks * kMx4ChunkBytes + 16 * q;
+    const uint32_t* ws = mx4_scales(Wq, N, K) + nr;
+    int m[FRAGS];
+#pragma unroll
+    for (int f = 0; f < FRAGS; ++f) m[f] = min(m0 + 16 * f + r, M - 1);
+    v4f acc[FRAGS];
+#pragma unroll
+    for (int f = 0; f < FRAGS; ++f) acc[f] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+    auto operand = [](uint4 p) { return v8i{(int)p.x, (int)p.y, (int)p.z, (int)p.w, 0, 0, 0, 0}; };
+    for (int c0 = wave; c0 < chunks; c0 += 4 * kMx4FewAhead) {
+        // (past the last chunk: its numbers once more, times weights of 0)
+        uint4 w[kMx4FewAhead], x[kMx4FewAhead][FRAGS];
+        uint32_t sw[kMx4FewAhead], sx[kMx4FewAhead][FRAGS];
+#pragma unroll
+        for (int u = 0; u < kMx4FewAhead; ++u) {
+            const int c = min(c0 + 4 * u, chunks - 1);
+            w[u] = *reinterpret_cast<const uint4*>(wrow + (size_t)c * kMx4ChunkBytes);
+            sw[u] = ws[(size_t)c * N] >> (8 * q);
+        }
+        if constexpr (REALX) {
+            float v[kMx4FewAhead][FRAGS][4][8];
+#pragma unroll
+            for (int u = 0; u < kMx4FewAhead; ++u)
+#pragma unroll
+                for (int f = 0; f < FRAGS; ++f)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        mx4_load8<VEC>(static_cast<const float*>(X), M, K, m[f], min(c0 + 4 * u, chunks - 1) * kMx4Chunk + 32 * q + 8 * i, v[u][f][i]);
+#pragma unroll
+            for (int u = 0; u < kMx4FewAhead; ++u)
+#pragma unroll
+                for (int f = 0; f < FRAGS; ++f) {
+                    const float(&b)[4][8] = v[u][f];
+                    const uint32_t e = mx_scale<MxE2M1>(max(max(mx4_top8(b[0]), mx4_top8(b[1])), max(mx4_top8(b[2]), mx4_top8(b[3]))));
+                    x[u][f] = make_uint4(mx4_nearest8(b[0], e), mx4_nearest8(b[1], e), mx4_nearest8(b[2], e), mx4_nearest8(b[3], e));
+                    sx[u][f] = e;
+                }
+        } else {
+            const unsigned char* xc = static_cast<const unsigned char*>(X) + 16 * q;
+            const uint32_t* xs = mx4_scales(X, M, K);
+#pragma unroll
+            for (int u = 0; u < kMx4FewAhead; ++u) {
+                const int c = min(c0 + 4 * u, chunks - 1);
+#pragma unroll
+                for (int f = 0; f < FRAGS; ++f) {
+                    x[u][f] = *reinterpret_cast<const uint4*>(xc + ((size_t)m[f] * chunks + c) * kMx4ChunkBytes);
+                    sx[u][f] = xs[(size_t)c * M + m[f]] >> (8 * q);
+                }
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < kMx4FewAhead; ++u) {
+            const uint4 wu = c0 + 4 * u < chunks ? w[u] : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+            for (int f = 0; f < FRAGS; ++f)
+                acc[f] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(operand(wu), operand(x[u][f]), acc[f], 4, 4, 0, (int)sw[u], 0, (int)sx[u][f]);
+        }
+    }
+#pragma unroll
+    for (int f = 0; f < FRAGS; ++f) part[wave][f][lane] = acc[f];
+    __syncthreads();
+    if (wave >= FRAGS) return;
+    // wave f finishes fragment f: register v of lane (r, q) is output n0 + 4 q + v of frame m0 + 16 f + r
+    const v4f sum = ((part[0][wave][lane] + part[1][wave][lane]) + part[2][wave][lane]) + part[3][wave][lane];
+    const int n = n0 + 4 * q, mf = m0 + 16 * wave + r;
+    if constexpr (ACT == ACT_SIGN) {
+        uint32_t bits = 0;
+#pragma unroll
+        for (int v = 0; v < 4; ++v) bits |= n + v < N && sign_bit(sum[v] + (bias ? bias[n + v] : 0.0f)) ? 1u << (4 * q + v) : 0u;
+        bits |= (uint32_t)__shfl_xor((int)bits, 16, kWave);
+        bits |= (uint32_t)__shfl_xor((int)bits, 32, kWave);
+        if (q == 0 && mf < M) static_cast<uint16_t*>(Y)[(size_t)mf * (2 * (size_t)yw32) + blockIdx.x] = (uint16_t)bits;
+    } else if (mf < M) {
+        float* y = static_cast<float*>(Y) + (size_t)mf * N + n;
+#pragma unroll
+        for (int v = 0; v < 4; ++v)
+            if (n + v < N) y[v] = mx4_act<ACT>(sum[v] + (bias ? bias[n + v] : 0.0f));
+    }
+}
+
 }  // namespace bnn
