@@ -50,12 +50,19 @@ int64_t fill(AdamwTable& table, const bnn_adamw_tensor* tensors, int n, int& nex
         const int64_t c = (tensors[next].count + kAdamwChunk - 1) / kAdamwChunk;
         if (c == 0) continue;
         if (chunks + c > kMaxCount / kAdamwChunk) break;   // (never a tensor by itself)
-        AdamwTensor& t = table.t[table.n++];
-        t = entry(next);
-        t.first = (int32_t)chunks;
+        table.first[table.n] = (int32_t)chunks;
+        table.t[table.n++] = entry(next);
         chunks += c;
     }
     return chunks;
+}
+
+// Tensors whose arrays the last level of cache (256 MB) does not hold beside each other are read and written past the caches: 29 million elements
+// 157 -> 141 us, with 8-bit states 107 -> 88, reading those back 51 -> 43; 1.3 million 8.9 and 9.6.
+bool past_caches(const bnn_adamw_tensor* tensors, int n) {
+    int64_t elements = 0;
+    for (int i = 0; i < n; ++i) elements += tensors[i].count;
+    return elements >= (int64_t)8 << 20;
 }
 
 int ranges_of(const bnn_adamw_tensor& t, int bits, Range* r) {
@@ -90,7 +97,11 @@ BNN_EXPORT int bnn_update_adamw(const bnn_adamw_tensor* tensors, int n_tensors, 
         if (const int rc = check_tensor(tensors[i], p.state_bits); rc != BNN_OK) return rc;
 
     // The tensors of one launch are updated side by side: what it writes must lie apart.  Checked for every launch before the first.
-    const AdamwParams kp{p.lr, p.beta1, p.beta2, p.eps, p.weight_decay, p.step, p.lr_at, p.step_at, seed_key(p.seed)};
+    const bool on_device = p.lr_at || p.step_at;
+    const AdamwParams kp{p.lr, p.beta1, p.beta2, p.eps, p.weight_decay, p.step, p.lr_at, p.step_at};
+    const AdamwFactors kf = on_device ? AdamwFactors{} : adamw_factors(p.lr, p.beta1, p.beta2, p.eps, p.weight_decay, p.step);
+    const uint32_t key = seed_key(p.seed);
+    const bool past = past_caches(tensors, n_tensors);
     for (int pass = 0; pass < 2; ++pass) {
         for (int next = 0, at = 0; next < n_tensors;) {
             AdamwTable table;
@@ -101,7 +112,7 @@ BNN_EXPORT int bnn_update_adamw(const bnn_adamw_tensor* tensors, int n_tensors, 
                 const bnn_adamw_tensor& t = tensors[i];
                 if (pass == 0) k += ranges_of(t, p.state_bits, ranges + k);
                 const bool vec = aligned(t.w, 16) && aligned(t.g, 16) && (p.state_bits == 32 ? aligned(t.m, 16) && aligned(t.v, 16) : aligned(t.m, 4) && aligned(t.v, 4));
-                return AdamwTensor{t.w, t.g, t.m, t.v, t.m_scale, t.v_scale, t.count, 0, (t.clip ? 1 : 0) | (vec ? 2 : 0)};
+                return AdamwTensor{t.w, t.g, t.m, t.v, t.m_scale, t.v_scale, t.count, t.clip, vec};
             });
             if (chunks == 0) break;
             at += table.n;
@@ -112,8 +123,18 @@ BNN_EXPORT int bnn_update_adamw(const bnn_adamw_tensor* tensors, int n_tensors, 
                 continue;
             }
             hipStream_t st = static_cast<hipStream_t>(stream);
-            if (p.state_bits == 32) adamw_kernel<32><<<(unsigned)chunks, 256, 0, st>>>(table, kp);
-            else adamw_kernel<8><<<(unsigned)chunks, 256, 0, st>>>(table, kp);
+            auto go = [&](auto bits, auto past) {
+                constexpr int B = decltype(bits)::value;
+                constexpr bool P = decltype(past)::value;
+                if (on_device) adamw_kernel<B, P, AdamwParams><<<(unsigned)chunks, 256, 0, st>>>(kp, key, table);
+                else adamw_kernel<B, P, AdamwFactors><<<(unsigned)chunks, 256, 0, st>>>(kf, key, table);
+            };
+            using I32 = std::integral_constant<int, 32>;
+            using I8 = std::integral_constant<int, 8>;
+            if (p.state_bits == 32 && past) go(I32{}, std::true_type{});
+            else if (p.state_bits == 32) go(I32{}, std::false_type{});
+            else if (past) go(I8{}, std::true_type{});
+            else go(I8{}, std::false_type{});
             if (const int rc = launch_status(); rc != BNN_OK) return rc;
         }
     }
@@ -147,14 +168,16 @@ BNN_EXPORT int bnn_unpack_adamw_states(const bnn_adamw_tensor* tensors, int n_te
                         if (o) ranges[k++] = {reinterpret_cast<uintptr_t>(o), reinterpret_cast<uintptr_t>(o) + 4 * (size_t)t.count, true};
                 }
                 const bool vec = aligned(mo, 16) && aligned(vo, 16) && aligned(t.m, 4) && aligned(t.v, 4);
-                return AdamwTensor{mo, vo, t.m, t.v, t.m_scale, t.v_scale, t.count, 0, vec ? 2 : 0};
+                return AdamwTensor{mo, vo, t.m, t.v, t.m_scale, t.v_scale, t.count, 0, vec};
             });
             if (chunks == 0) break;
             if (pass == 0) {
                 if (!apart(ranges, k)) return BNN_EINVAL;
                 continue;
             }
-            adamw_unpack_kernel<<<(unsigned)chunks, 256, 0, static_cast<hipStream_t>(stream)>>>(table);
+            hipStream_t st = static_cast<hipStream_t>(stream);
+            if (past_caches(tensors, n_tensors)) adamw_unpack_kernel<true><<<(unsigned)chunks, 256, 0, st>>>(table);
+            else adamw_unpack_kernel<false><<<(unsigned)chunks, 256, 0, st>>>(table);
             if (const int rc = launch_status(); rc != BNN_OK) return rc;
         }
     }

@@ -8,7 +8,7 @@
 
 namespace bnn {
 
-constexpr int kAdamwTensors = 40;      // of one launch: 64 bytes of its arguments each
+constexpr int kAdamwTensors = 40;      // of one launch, in its arguments
 constexpr int kAdamwChunk = 4096;      // elements that a workgroup takes: 4 quads a thread
 
 struct AdamwTensor {
@@ -17,12 +17,12 @@ struct AdamwTensor {
     void *m, *v;
     unsigned char *m_scale, *v_scale;
     int64_t count;
-    int32_t first;     // number of the tensor's first chunk in the launch
-    int32_t flags;     // bit 0: clip, bit 1: 16-byte (8-bit states: codes 4-byte) accesses
+    int32_t clip, vec;     // vec: 16-byte accesses, 4-byte ones of 8-bit codes
 };
 struct AdamwTable {
+    int32_t n, at;                     // tensors; how many tensors with elements the call has had in earlier launches
+    int32_t first[kAdamwTensors];      // number of the tensor's first chunk in the launch
     AdamwTensor t[kAdamwTensors];
-    int n, at;         // tensors; how many tensors with elements the call has had in earlier launches
 };
 
 // beta^t by squaring: the same multiplications on the host and on the device
@@ -39,159 +39,220 @@ __host__ __device__ inline AdamwFactors adamw_factors(double lr, double beta1, d
     return {(float)beta1, (float)(1.0 - beta1), (float)beta2, (float)(1.0 - beta2), (float)eps, (float)(lr * weight_decay),
             (float)(lr / (1.0 - power(beta1, step))), (float)(1.0 / sqrt(1.0 - power(beta2, step)))};
 }
+// Hyperparameters of a call that has some of them on the device: the factors are then made by every workgroup.
 struct AdamwParams {
     double lr, beta1, beta2, eps, weight_decay;
     int64_t step;
     const float* lr_at;
     const int64_t* step_at;
-    uint32_t key;
+    __device__ AdamwFactors factors() const {
+        const int64_t t = step_at ? *step_at : step;
+        return adamw_factors(lr_at ? (double)*lr_at : lr, beta1, beta2, eps, weight_decay, t > 1 ? t : 1);
+    }
 };
+__device__ __forceinline__ AdamwFactors factors_of(const AdamwFactors& f) { return f; }
+__device__ __forceinline__ AdamwFactors factors_of(const AdamwParams& p) { return p.factors(); }
 
-// the tensor that a chunk belongs to
+// The tensor that a chunk belongs to: the last one whose first chunk is not behind it.  (A lane per tensor: the arguments are far from the CUs,
+// and looking them through one by one would wait for them as often.)
 __device__ __forceinline__ int adamw_tensor_of(const AdamwTable& table, int chunk) {
-    int i = 0;
-    while (i + 1 < table.n && table.t[i + 1].first <= chunk) ++i;
-    return i;
+    static_assert(kAdamwTensors <= kWave, "a lane per tensor");
+    const int lane = lane_id();
+    return __builtin_popcountll(__builtin_amdgcn_ballot_w64(lane < table.n && table.first[lane < table.n ? lane : 0] <= chunk)) - 1;
 }
 
 struct Quad { float v[4]; };
-__device__ __forceinline__ Quad load_quad(const float* p, int64_t e, int64_t count, bool vec) {
-    Quad q;
-    if (vec && e + 4 <= count) {
-        const float4 f = *reinterpret_cast<const float4*>(p + e);
-        q.v[0] = f.x; q.v[1] = f.y; q.v[2] = f.z; q.v[3] = f.w;
-    } else {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) q.v[j] = e + j < count ? p[e + j] : 0.0f;
+// How a thread reaches its elements.  WHOLE: the chunk lies inside the tensor and its arrays are aligned; otherwise every access looks at both.
+// PAST: fp32 past the caches, for tensors that they do not hold (codes, a quarter of the size, stay).
+template <bool WHOLE, bool PAST>
+struct AdamwAccess {
+    typedef float v4f __attribute__((ext_vector_type(4)));
+    template <class T>
+    static __device__ __forceinline__ T get(const T* p) {
+        if constexpr (PAST) return __builtin_nontemporal_load(p);
+        else return *p;
     }
-    return q;
-}
-__device__ __forceinline__ void store_quad(float* p, int64_t e, int64_t count, bool vec, const Quad& q) {
-    if (vec && e + 4 <= count) {
-        *reinterpret_cast<float4*>(p + e) = make_float4(q.v[0], q.v[1], q.v[2], q.v[3]);
-    } else {
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-            if (e + j < count) p[e + j] = q.v[j];
+    template <class T>
+    static __device__ __forceinline__ void put(T* p, T v) {
+        if constexpr (PAST) __builtin_nontemporal_store(v, p);
+        else *p = v;
     }
-}
-// 4 codes, one byte each
-__device__ __forceinline__ uint32_t load_codes(const unsigned char* p, int64_t e, int64_t count, bool vec) {
-    if (vec && e + 4 <= count) return *reinterpret_cast<const uint32_t*>(p + e);
-    uint32_t c = 0;
+    static __device__ __forceinline__ Quad load(const float* p, int64_t e, int64_t count, bool vec) {
+        Quad q;
+        if (WHOLE || (vec && e + 4 <= count)) {
+            const v4f f = get(reinterpret_cast<const v4f*>(p + e));
+            q.v[0] = f[0]; q.v[1] = f[1]; q.v[2] = f[2]; q.v[3] = f[3];
+        } else {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) c |= e + j < count ? (uint32_t)p[e + j] << (8 * j) : 0u;
-    return c;
-}
-__device__ __forceinline__ void store_codes(unsigned char* p, int64_t e, int64_t count, bool vec, uint32_t c) {
-    if (vec && e + 4 <= count) {
-        *reinterpret_cast<uint32_t*>(p + e) = c;
-    } else {
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-            if (e + j < count) p[e + j] = (unsigned char)(c >> (8 * j));
+            for (int j = 0; j < 4; ++j) q.v[j] = e + j < count ? p[e + j] : 0.0f;
+        }
+        return q;
     }
-}
+    static __device__ __forceinline__ void store(float* p, int64_t e, int64_t count, bool vec, const Quad& q) {
+        if (WHOLE || (vec && e + 4 <= count)) {
+            put(reinterpret_cast<v4f*>(p + e), v4f{q.v[0], q.v[1], q.v[2], q.v[3]});
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (e + j < count) p[e + j] = q.v[j];
+        }
+    }
+    // 4 codes, one byte each
+    static __device__ __forceinline__ uint32_t load_codes(const unsigned char* p, int64_t e, int64_t count, bool vec) {
+        if (WHOLE || (vec && e + 4 <= count)) return *reinterpret_cast<const uint32_t*>(p + e);
+        uint32_t c = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) c |= e + j < count ? (uint32_t)p[e + j] << (8 * j) : 0u;
+        return c;
+    }
+    static __device__ __forceinline__ void store_codes(unsigned char* p, int64_t e, int64_t count, bool vec, uint32_t c) {
+        if (WHOLE || (vec && e + 4 <= count)) {
+            *reinterpret_cast<uint32_t*>(p + e) = c;
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (e + j < count) p[e + j] = (unsigned char)(c >> (8 * j));
+        }
+    }
+};
 
 __device__ __forceinline__ float signed_code(uint32_t c, int j) { return (float)(int8_t)(c >> (8 * j)); }
 __device__ __forceinline__ float unsigned_code(uint32_t c, int j) { return (float)((c >> (8 * j)) & 0xFFu); }
 
 // The update, every operation rounded in fp32 (no contraction: the library is built with -ffp-contract=off):
 //     m' = b1 m + c1 g,   v' = b2 v + (c2 g) g,   r = sqrt(v'),   w' = w - (decay w + (size m') / (r q + eps))
-template <int BITS>
-__global__ __launch_bounds__(256) void adamw_kernel(const AdamwTable table, const AdamwParams p) {
-    const int i = adamw_tensor_of(table, (int)blockIdx.x);
-    const AdamwTensor& t = table.t[i];
-    const AdamwFactors f = adamw_factors(p.lr_at ? (double)*p.lr_at : p.lr, p.beta1, p.beta2, p.eps, p.weight_decay,
-                                         p.step_at ? (*p.step_at > 1 ? *p.step_at : 1) : p.step);
-    const bool clip = t.flags & 1, vec = t.flags & 2;
-    const int64_t chunk = (int64_t)((int)blockIdx.x - t.first) * kAdamwChunk;
-    const uint32_t key = mix32(p.key + (uint32_t)(table.at + i));
+// Bound by memory: a thread requests all of its four quads before it uses the first.
+template <int BITS, bool WHOLE, bool PAST>
+__device__ __forceinline__ void adamw_chunk(const AdamwTensor& t, const AdamwFactors& f, uint32_t key, int64_t chunk) {
+    using A = AdamwAccess<WHOLE, PAST>;
+    constexpr int kQuads = kAdamwChunk / 1024;
+    Quad w[kQuads], g[kQuads], m[kQuads], v[kQuads];
+    uint32_t cm[kQuads], cv[kQuads], em[kQuads], ev[kQuads];
+    const int64_t e0 = chunk + (int)threadIdx.x * 4;
+    auto inside = [&](int64_t e) { return WHOLE || (e & ~31) < t.count; };   // (whole groups of the 8 lanes of a block)
 #pragma unroll
-    for (int k = 0; k < kAdamwChunk / 1024; ++k) {
-        const int64_t e = chunk + k * 1024 + (int)threadIdx.x * 4;
-        if ((e & ~31) >= t.count) break;   // whole groups of 8 lanes
-        Quad w = load_quad(t.w, e, t.count, vec), m, v, r;
-        const Quad g = load_quad(t.g, e, t.count, vec);
+    for (int k = 0; k < kQuads; ++k) {
+        const int64_t e = e0 + 1024 * k;
+        if (!inside(e)) break;
+        w[k] = A::load(t.w, e, t.count, t.vec);
+        g[k] = A::load(t.g, e, t.count, t.vec);
         if constexpr (BITS == 32) {
-            m = load_quad(static_cast<const float*>(t.m), e, t.count, vec);
-            v = load_quad(static_cast<const float*>(t.v), e, t.count, vec);
+            m[k] = A::load(static_cast<const float*>(t.m), e, t.count, t.vec);
+            v[k] = A::load(static_cast<const float*>(t.v), e, t.count, t.vec);
         } else {
-            const uint32_t cm = load_codes(static_cast<const unsigned char*>(t.m), e, t.count, vec);
-            const uint32_t cv = load_codes(static_cast<const unsigned char*>(t.v), e, t.count, vec);
-            const float sm = mx_scale_value(t.m_scale[e >> 5]), sv = mx_scale_value(t.v_scale[e >> 5]);
+            cm[k] = A::load_codes(static_cast<const unsigned char*>(t.m), e, t.count, t.vec);
+            cv[k] = A::load_codes(static_cast<const unsigned char*>(t.v), e, t.count, t.vec);
+            em[k] = t.m_scale[e >> 5];
+            ev[k] = t.v_scale[e >> 5];
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < kQuads; ++k) {
+        const int64_t e = e0 + 1024 * k;
+        if (!inside(e)) break;
+        Quad r;
+        if constexpr (BITS == 8) {
+            const float sm = mx_scale_value(em[k]), sv = mx_scale_value(ev[k]);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                m.v[j] = signed_code(cm, j) * sm;
-                const float old = unsigned_code(cv, j) * sv;
-                v.v[j] = old * old;
+                m[k].v[j] = signed_code(cm[k], j) * sm;
+                const float old = unsigned_code(cv[k], j) * sv;
+                v[k].v[j] = old * old;
             }
         }
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            m.v[j] = f.b1 * m.v[j] + f.c1 * g.v[j];
-            v.v[j] = f.b2 * v.v[j] + (f.c2 * g.v[j]) * g.v[j];
-            r.v[j] = __builtin_sqrtf(v.v[j]);
-            w.v[j] = w.v[j] - (f.decay * w.v[j] + (f.size * m.v[j]) / (r.v[j] * f.q + f.eps));
-            if (clip) w.v[j] = hardtanh(w.v[j]);
+            const float gj = g[k].v[j];
+            m[k].v[j] = f.b1 * m[k].v[j] + f.c1 * gj;
+            v[k].v[j] = f.b2 * v[k].v[j] + (f.c2 * gj) * gj;
+            r.v[j] = __builtin_sqrtf(v[k].v[j]);
+            const float wj = w[k].v[j], n = wj - (f.decay * wj + (f.size * m[k].v[j]) / (r.v[j] * f.q + f.eps));
+            w[k].v[j] = t.clip ? hardtanh(n) : n;
         }
-        store_quad(t.w, e, t.count, vec, w);
+        A::store(t.w, e, t.count, t.vec, w[k]);
         if constexpr (BITS == 32) {
-            store_quad(static_cast<float*>(t.m), e, t.count, vec, m);
-            store_quad(static_cast<float*>(t.v), e, t.count, vec, v);
+            A::store(static_cast<float*>(t.m), e, t.count, t.vec, m[k]);
+            A::store(static_cast<float*>(t.v), e, t.count, t.vec, v[k]);
         } else {
             uint32_t tm = 0, tv = 0;   // (elements past the end are 0)
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                tm = max(tm, __float_as_uint(m.v[j]) & 0x7FFFFFFFu);
+                tm = max(tm, __float_as_uint(m[k].v[j]) & 0x7FFFFFFFu);
                 tv = max(tv, __float_as_uint(r.v[j]) & 0x7FFFFFFFu);
             }
-            const uint32_t em = mx_scale<MxInt8>(max_of_8_lanes(tm)), ev = mx_scale<MxUint8>(max_of_8_lanes(tv));
-            const float im = mx_inverse_scale(em), iv = mx_inverse_scale(ev);
+            const uint32_t nm = mx_scale<MxInt8>(max_of_8_lanes(tm)), nv = mx_scale<MxUint8>(max_of_8_lanes(tv));
+            const float im = mx_inverse_scale(nm), iv = mx_inverse_scale(nv);
             const uint32_t block_key = mix32(key + (uint32_t)(e >> 5));
-            uint32_t cm = 0, cv = 0;
+            uint32_t am = 0, av = 0;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const uint32_t h = mix32(block_key + (uint32_t)((e & 31) + j));
-                const int am = (int)(__builtin_fabsf(m.v[j]) * im + (float)(h & 0xFFFFu) * 0x1p-16f);
-                const int av = (int)(r.v[j] * iv + (float)(h >> 16) * 0x1p-16f);
-                cm |= ((uint32_t)(m.v[j] < 0.0f ? -am : am) & 0xFFu) << (8 * j);
-                cv |= ((uint32_t)av & 0xFFu) << (8 * j);
+                const int cmj = (int)(__builtin_fabsf(m[k].v[j]) * im + (float)(h & 0xFFFFu) * 0x1p-16f);
+                const int cvj = (int)(r.v[j] * iv + (float)(h >> 16) * 0x1p-16f);
+                am |= ((uint32_t)(m[k].v[j] < 0.0f ? -cmj : cmj) & 0xFFu) << (8 * j);
+                av |= ((uint32_t)cvj & 0xFFu) << (8 * j);
             }
-            if (em == 255) cm = 0;
-            if (ev == 255) cv = 0;
-            store_codes(static_cast<unsigned char*>(t.m), e, t.count, vec, cm);
-            store_codes(static_cast<unsigned char*>(t.v), e, t.count, vec, cv);
+            A::store_codes(static_cast<unsigned char*>(t.m), e, t.count, t.vec, nm == 255 ? 0u : am);
+            A::store_codes(static_cast<unsigned char*>(t.v), e, t.count, t.vec, nv == 255 ? 0u : av);
             if ((threadIdx.x & 7) == 0) {
-                t.m_scale[e >> 5] = (unsigned char)em;
-                t.v_scale[e >> 5] = (unsigned char)ev;
+                t.m_scale[e >> 5] = (unsigned char)nm;
+                t.v_scale[e >> 5] = (unsigned char)nv;
             }
         }
     }
 }
 
+// HYPER: AdamwFactors, or AdamwParams where some of them are read on the device.
+template <int BITS, bool PAST, class HYPER>
+__global__ __launch_bounds__(256) void adamw_kernel(const HYPER hyper, uint32_t seed, const AdamwTable table) {
+    const int i = adamw_tensor_of(table, (int)blockIdx.x);
+    const AdamwTensor t = table.t[i];
+    const AdamwFactors f = factors_of(hyper);
+    const int64_t chunk = (int64_t)((int)blockIdx.x - table.first[i]) * kAdamwChunk;
+    const uint32_t key = mix32(seed + (uint32_t)(table.at + i));
+    if (t.vec && chunk + kAdamwChunk <= t.count) adamw_chunk<BITS, true, PAST>(t, f, key, chunk);
+    else adamw_chunk<BITS, false, PAST>(t, f, key, chunk);
+}
+
 // 8-bit states as the numbers they stand for.  In the table w is where m goes (may be absent) and g where v goes.
-__global__ __launch_bounds__(256) void adamw_unpack_kernel(const AdamwTable table) {
-    const AdamwTensor& t = table.t[adamw_tensor_of(table, (int)blockIdx.x)];
-    const int64_t chunk = (int64_t)((int)blockIdx.x - t.first) * kAdamwChunk;
-    const bool vec = t.flags & 2;
+template <bool WHOLE, bool PAST>
+__device__ __forceinline__ void adamw_unpack_chunk(const AdamwTensor& t, int64_t chunk) {
+    using A = AdamwAccess<WHOLE, PAST>;
+    constexpr int kQuads = kAdamwChunk / 1024;
+    uint32_t cm[kQuads], cv[kQuads], em[kQuads], ev[kQuads];
+    const int64_t e0 = chunk + (int)threadIdx.x * 4;
 #pragma unroll
-    for (int k = 0; k < kAdamwChunk / 1024; ++k) {
-        const int64_t e = chunk + k * 1024 + (int)threadIdx.x * 4;
-        if (e >= t.count) break;
-        const uint32_t cm = load_codes(static_cast<const unsigned char*>(t.m), e, t.count, vec);
-        const uint32_t cv = load_codes(static_cast<const unsigned char*>(t.v), e, t.count, vec);
-        const float sm = mx_scale_value(t.m_scale[e >> 5]), sv = mx_scale_value(t.v_scale[e >> 5]);
+    for (int k = 0; k < kQuads; ++k) {
+        const int64_t e = e0 + 1024 * k;
+        if (!WHOLE && e >= t.count) break;
+        cm[k] = A::load_codes(static_cast<const unsigned char*>(t.m), e, t.count, t.vec);
+        cv[k] = A::load_codes(static_cast<const unsigned char*>(t.v), e, t.count, t.vec);
+        em[k] = t.m_scale[e >> 5];
+        ev[k] = t.v_scale[e >> 5];
+    }
+#pragma unroll
+    for (int k = 0; k < kQuads; ++k) {
+        const int64_t e = e0 + 1024 * k;
+        if (!WHOLE && e >= t.count) break;
+        const float sm = mx_scale_value(em[k]), sv = mx_scale_value(ev[k]);
         Quad m, v;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            m.v[j] = signed_code(cm, j) * sm;
-            const float r = unsigned_code(cv, j) * sv;
+            m.v[j] = signed_code(cm[k], j) * sm;
+            const float r = unsigned_code(cv[k], j) * sv;
             v.v[j] = r * r;
         }
-        if (t.w) store_quad(t.w, e, t.count, vec, m);
-        if (t.g) store_quad(const_cast<float*>(t.g), e, t.count, vec, v);
+        if (t.w) A::store(t.w, e, t.count, t.vec, m);
+        if (t.g) A::store(const_cast<float*>(t.g), e, t.count, t.vec, v);
     }
+}
+template <bool PAST>
+__global__ __launch_bounds__(256) void adamw_unpack_kernel(const AdamwTable table) {
+    const int i = adamw_tensor_of(table, (int)blockIdx.x);
+    const AdamwTensor t = table.t[i];
+    const int64_t chunk = (int64_t)((int)blockIdx.x - table.first[i]) * kAdamwChunk;
+    if (t.vec && chunk + kAdamwChunk <= t.count) adamw_unpack_chunk<true, PAST>(t, chunk);
+    else adamw_unpack_chunk<false, PAST>(t, chunk);
 }
 
 }  // namespace bnn
