@@ -115,6 +115,40 @@ __device__ __forceinline__ bool front_of_run(const Clear& c, const Pull& p) {
 // Eq. 3 of the paper: +1 exactly when v > 0 (0, -0 and NaN give -1, i.e. bit 0).
 __device__ __forceinline__ bool sign_bit(float v) { return v > 0.0f; }
 
+// 32 x 32 bits across the 32 lanes of a half wave: afterwards bit j of lane i is what bit i of lane j was.  Five exchanges with
+// the lane whose number differs in one bit; a lane keeps the half of its bits that stays and takes the other one rotated.
+struct TransposeBits {
+    uint32_t keep[5], rot[5];
+    __device__ __forceinline__ explicit TransposeBits(int lane) {
+        constexpr uint32_t kLow[5] = {0x0000FFFFu, 0x00FF00FFu, 0x0F0F0F0Fu, 0x33333333u, 0x55555555u};
+#pragma unroll
+        for (int t = 0; t < 5; ++t) {
+            const int s = 16 >> t;
+            keep[t] = (lane & s) ? ~kLow[t] : kLow[t];
+            rot[t] = (lane & s) ? (uint32_t)s : (uint32_t)(32 - s);   // to the right
+        }
+    }
+    template <int S>
+    static __device__ __forceinline__ uint32_t partner(uint32_t v) {
+        return (uint32_t)__builtin_amdgcn_ds_swizzle((int)v, 0x1F | (S << 10));
+    }
+    template <int T, int N>
+    __device__ __forceinline__ void step(uint32_t (&w)[N]) const {
+        uint32_t p[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) p[i] = partner<(16 >> T)>(w[i]);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const uint32_t o = __builtin_amdgcn_alignbit(p[i], p[i], rot[T]);
+            w[i] = (w[i] & keep[T]) | (o & ~keep[T]);
+        }
+    }
+    template <int N>
+    __device__ __forceinline__ void run(uint32_t (&w)[N]) const {
+        step<0>(w); step<1>(w); step<2>(w); step<3>(w); step<4>(w);
+    }
+};
+
 // Eq. 1 with the per-layer scale: one fused multiply-add, a single rounding.
 __device__ __forceinline__ float affine(float scale, float v, float bias) { return __builtin_fmaf(scale, v, bias); }
 

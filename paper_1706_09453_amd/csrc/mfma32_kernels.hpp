@@ -83,40 +83,6 @@ __device__ __forceinline__ SignColumn sign_column(float scale, float bias, float
     return {wide ? -scale : -scale * unit, 0.0f - (wide && __builtin_fabsf(bias) >= 1.0f ? bias / unit : bias)};
 }
 
-// 32 x 32 bits across the 32 lanes of a half wave: afterwards bit j of lane i is what bit i of lane j was.  Five exchanges with
-// the lane whose number differs in one bit; a lane keeps the half of its bits that stays and takes the other one rotated.
-struct TransposeBits {
-    uint32_t keep[5], rot[5];
-    __device__ __forceinline__ explicit TransposeBits(int lane) {
-        constexpr uint32_t kLow[5] = {0x0000FFFFu, 0x00FF00FFu, 0x0F0F0F0Fu, 0x33333333u, 0x55555555u};
-#pragma unroll
-        for (int t = 0; t < 5; ++t) {
-            const int s = 16 >> t;
-            keep[t] = (lane & s) ? ~kLow[t] : kLow[t];
-            rot[t] = (lane & s) ? (uint32_t)s : (uint32_t)(32 - s);   // to the right
-        }
-    }
-    template <int S>
-    static __device__ __forceinline__ uint32_t partner(uint32_t v) {
-        return (uint32_t)__builtin_amdgcn_ds_swizzle((int)v, 0x1F | (S << 10));
-    }
-    template <int T, int N>
-    __device__ __forceinline__ void step(uint32_t (&w)[N]) const {
-        uint32_t p[N];
-#pragma unroll
-        for (int i = 0; i < N; ++i) p[i] = partner<(16 >> T)>(w[i]);
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const uint32_t o = __builtin_amdgcn_alignbit(p[i], p[i], rot[T]);
-            w[i] = (w[i] & keep[T]) | (o & ~keep[T]);
-        }
-    }
-    template <int N>
-    __device__ __forceinline__ void run(uint32_t (&w)[N]) const {
-        step<0>(w); step<1>(w); step<2>(w); step<3>(w); step<4>(w);
-    }
-};
-
 // Called inside the product loop, after the first products: the loads that produced sc/bi then stay in front of
 // the loop, where they were written, instead of moving next to their use in the epilogue, and by the time this
 // point is reached they have long returned (the operand words used by those products were requested later).

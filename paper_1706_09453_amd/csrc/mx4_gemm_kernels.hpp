@@ -185,6 +185,32 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, FM * FN > 8 ? 1 : 2) void m
     // register v of lane (r, g): row 8 (v / 4) + 4 g + v % 4, column r.  Stores go through a buffer that begins at the fragment's first row and
     // ends with the matrix, so that rows past M fall away; columns past N get an offset past its end.
     const float* bias_s = reinterpret_cast<const float*>(mx4_mem + STAGES * T::kStage) + wn * (32 * FN) + r;
+    if constexpr (ACT == ACT_SIGN) {
+        // A lane gathers the bits of its column over the rows of two fragments, and the 32 x 32 bits of a half wave are transposed: a word per lane.
+        static_assert(FN <= 2, "TransposeBits takes what a lane stores together");
+        const TransposeBits transposed(lane);
+#pragma unroll
+        for (int p = 0; p < (FM + 1) / 2; ++p) {
+            uint32_t w[FN];
+#pragma unroll
+            for (int j = 0; j < FN; ++j) {
+                const float b = bias ? bias_s[32 * j] : 0.0f;
+                w[j] = 0u;
+#pragma unroll
+                for (int i = 0; i < (FM > 1 ? 32 : 16); ++i)   // bit i: row 8 (v / 4) + 4 g + v % 4 of fragment 2 p + i / 16, v = i % 16
+                    w[j] |= sign_bit(acc[2 * p + (i >> 4)][j][i & 15] + b) ? 1u << i : 0u;
+                w[j] = n_base + 32 * j + r < N ? w[j] : 0u;
+            }
+            transposed.run(w);
+            const int v = r & 15, m = m_base + (2 * p + (r >> 4)) * 32 + 8 * (v >> 2) + 4 * g + (v & 3);
+            if (m < M && (FM > 1 || r < 16)) {
+#pragma unroll
+                for (int j = 0; j < FN; ++j)
+                    if ((n_base >> 5) + j < yw32) static_cast<uint32_t*>(Y)[(size_t)m * yw32 + (n_base >> 5) + j] = w[j];
+            }
+        }
+        return;
+    }
 #pragma unroll
     for (int j = 0; j < FN; ++j) {
         const int n = n_base + 32 * j + r;
@@ -192,28 +218,19 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, FM * FN > 8 ? 1 : 2) void m
 #pragma unroll
         for (int i = 0; i < FM; ++i) {
             const int m = m_base + 32 * i;
-            if constexpr (ACT == ACT_SIGN) {
+            const int stride = N * 4, rows = __builtin_amdgcn_readfirstlane(min(max(M - m, 0), 32));   // (32 rows of 2^22 columns: 2^29 bytes)
+            const uint64_t first = reinterpret_cast<uint64_t>(Y) + (size_t)min(m, M) * N * 4;
+            const uint64_t low = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)first), high = (uint32_t)__builtin_amdgcn_readfirstlane((int)(first >> 32));
+            const auto out = __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>(low | high << 32), 0, rows * stride, 0x00020000);
+            const int at = n < N ? 4 * g * stride + n * 4 : 0x7FFFFFFF;
+            auto store = [&](auto policy) {
 #pragma unroll
-                for (int v = 0; v < 16; ++v) {
-                    const unsigned long long bits = __builtin_amdgcn_ballot_w64(n < N && sign_bit(acc[i][j][v] + b));
-                    const int word = (n_base >> 5) + j, mv = m + 8 * (v >> 2) + 4 * g + (v & 3);
-                    if (r == 0 && mv < M && word < yw32) static_cast<uint32_t*>(Y)[(size_t)mv * yw32 + word] = (uint32_t)(bits >> (32 * g));
-                }
-            } else {
-                const int stride = N * 4, rows = __builtin_amdgcn_readfirstlane(min(max(M - m, 0), 32));   // (32 rows of 2^22 columns: 2^29 bytes)
-                const uint64_t first = reinterpret_cast<uint64_t>(Y) + (size_t)min(m, M) * N * 4;
-                const uint64_t low = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)first), high = (uint32_t)__builtin_amdgcn_readfirstlane((int)(first >> 32));
-                const auto out = __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>(low | high << 32), 0, rows * stride, 0x00020000);
-                const int at = n < N ? 4 * g * stride + n * 4 : 0x7FFFFFFF;
-                auto store = [&](auto policy) {
-#pragma unroll
-                    for (int v = 0; v < 16; ++v)
-                        __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(mx4_act<ACT>(acc[i][j][v] + b)), out, at, (8 * (v >> 2) + (v & 3)) * stride,
-                                                              decltype(policy)::value);
-                };
-                if (nt) store(std::integral_constant<int, 2>{});   // past the caches
-                else store(std::integral_constant<int, 0>{});
-            }
+                for (int v = 0; v < 16; ++v)
+                    __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(mx4_act<ACT>(acc[i][j][v] + b)), out, at, (8 * (v >> 2) + (v & 3)) * stride,
+                                                          decltype(policy)::value);
+            };
+            if (nt) store(std::integral_constant<int, 2>{});   // past the caches
+            else store(std::integral_constant<int, 0>{});
         }
     }
 }
