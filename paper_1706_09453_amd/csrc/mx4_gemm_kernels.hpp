@@ -211,27 +211,46 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, FM * FN > 8 ? 1 : 2) void m
         }
         return;
     }
+    // Two fragments side by side exchange half waves, so that a store writes 64 columns of one row (32 of two rows in pieces of a line each
+    // where rows are no whole lines: 8192 x 2048 x 3400 65 us, 54 so).
+    float b[FN];
 #pragma unroll
-    for (int j = 0; j < FN; ++j) {
-        const int n = n_base + 32 * j + r;
-        const float b = bias ? bias_s[32 * j] : 0.0f;
+    for (int j = 0; j < FN; ++j) b[j] = bias ? bias_s[32 * j] : 0.0f;
+    constexpr bool kPairs = FN % 2 == 0;
 #pragma unroll
-        for (int i = 0; i < FM; ++i) {
-            const int m = m_base + 32 * i;
-            const int stride = N * 4, rows = __builtin_amdgcn_readfirstlane(min(max(M - m, 0), 32));   // (32 rows of 2^22 columns: 2^29 bytes)
-            const uint64_t first = reinterpret_cast<uint64_t>(Y) + (size_t)min(m, M) * N * 4;
-            const uint64_t low = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)first), high = (uint32_t)__builtin_amdgcn_readfirstlane((int)(first >> 32));
-            const auto out = __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>(low | high << 32), 0, rows * stride, 0x00020000);
-            const int at = n < N ? 4 * g * stride + n * 4 : 0x7FFFFFFF;
-            auto store = [&](auto policy) {
+    for (int i = 0; i < FM; ++i) {
+        const int m = m_base + 32 * i;
+        const int stride = N * 4, rows = __builtin_amdgcn_readfirstlane(min(max(M - m, 0), 32));   // (32 rows of 2^22 columns: 2^29 bytes)
+        const uint64_t first = reinterpret_cast<uint64_t>(Y) + (size_t)min(m, M) * N * 4;
+        const uint64_t low = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)first), high = (uint32_t)__builtin_amdgcn_readfirstlane((int)(first >> 32));
+        const auto out = __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>(low | high << 32), 0, rows * stride, 0x00020000);
+        auto store = [&](auto policy) {
+            constexpr int P = decltype(policy)::value;
+            if constexpr (kPairs) {
 #pragma unroll
-                for (int v = 0; v < 16; ++v)
-                    __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(mx4_act<ACT>(acc[i][j][v] + b)), out, at, (8 * (v >> 2) + (v & 3)) * stride,
-                                                          decltype(policy)::value);
-            };
-            if (nt) store(std::integral_constant<int, 2>{});   // past the caches
-            else store(std::integral_constant<int, 0>{});
-        }
+                for (int j = 0; j < FN; j += 2) {
+                    const int n = n_base + 32 * j + lane, at = n < N ? n * 4 : 0x7FFFFFFF;
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) {
+                        const auto pair = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx4_act<ACT>(acc[i][j][v] + b[j])),
+                                                                           __float_as_uint(mx4_act<ACT>(acc[i][j + 1][v] + b[j + 1])), false, false);
+                        const int row = 8 * (v >> 2) + (v & 3);
+                        __builtin_amdgcn_raw_buffer_store_b32(pair[0], out, at, row * stride, P);
+                        __builtin_amdgcn_raw_buffer_store_b32(pair[1], out, at, (row + 4) * stride, P);
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < FN; ++j) {
+                    const int n = n_base + 32 * j + r, at = n < N ? 4 * g * stride + n * 4 : 0x7FFFFFFF;
+#pragma unroll
+                    for (int v = 0; v < 16; ++v)
+                        __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(mx4_act<ACT>(acc[i][j][v] + b[j])), out, at, (8 * (v >> 2) + (v & 3)) * stride, P);
+                }
+            }
+        };
+        if (nt) store(std::integral_constant<int, 2>{});   // past the caches
+        else store(std::integral_constant<int, 0>{});
     }
 }
 
