@@ -134,6 +134,8 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, FM * FN > 8 ? 1 : 2) void m
         (f < FN ? sb[f < FN ? f : 0] : sa[f < FN ? 0 : f - FN]) = q;
     };
     constexpr int F = FM + FN, P = FM * FN;   // fragments, products of a step
+    constexpr int kEach = (F + P - 1) / P, kBusy = (F + kEach - 1) / kEach;   // reads behind a product, products that have some
+    constexpr int kFrom = kBusy < P ? kBusy : P - 1, kRest = P - kFrom;       // products that loads follow: those behind the reads
     v8i a0[FM], b0[FN], a1[FM], b1[FN];
     int sa[FM], sb[FN], na[FM], nb[FN];
 #pragma unroll
@@ -155,7 +157,7 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, FM * FN > 8 ? 1 : 2) void m
             const int i = q / FN, j = q % FN;
             acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a0[i], b0[j], acc[i][j], 4, 4, 0, sa[i], 0, sb[j]);
 #pragma unroll
-            for (int f = q * F / P; f < (q + 1) * F / P; ++f) fetch_one(f, a1, b1, slot, p1);
+            for (int f = q * kEach; f < (q + 1) * kEach && f < F; ++f) fetch_one(f, a1, b1, slot, p1);
             __builtin_amdgcn_sched_barrier(0);
         }
         if constexpr (decltype(more)::value) turn();
@@ -166,13 +168,15 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, FM * FN > 8 ? 1 : 2) void m
             const int i = q / FN, j = q % FN;
             acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a1[i], b1[j], acc[i][j], 4, 4, 2, sa[i], 2, sb[j]);
 #pragma unroll
-            for (int f = q * F / P; f < (q + 1) * F / P; ++f) {
+            for (int f = q * kEach; f < (q + 1) * kEach && f < F; ++f) {
                 fetch_one(f, a0, b0, from, p0);
                 fetch_scale(f, na, nb, from);
             }
             if constexpr (decltype(more)::value) {
+                if (q >= kFrom) {
 #pragma unroll
-                for (int l = q * T::kLoads / P; l < (q + 1) * T::kLoads / P; ++l) request_one(l, c + STAGES, slot);
+                    for (int l = (q - kFrom) * T::kLoads / kRest; l < (q - kFrom + 1) * T::kLoads / kRest; ++l) request_one(l, c + STAGES, slot);
+                }
             }
             __builtin_amdgcn_sched_barrier(0);
         }
