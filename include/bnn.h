@@ -468,14 +468,20 @@ typedef enum bnn_rounding {
 
 /* From fp32 to 4 bits: X [R][C] along its rows (Q: a matrix [R][C]), along its columns (QT: X^T, a matrix [C][R]) or both, from one read.
  *   Q, QT  out, nullable, not both NULL
- *   seed   of the random bits of BNN_ROUND_STOCHASTIC (unused otherwise): the same seed gives the same codes.  Element (r, c) takes
+ *   seed   of the random bits of BNN_ROUND_STOCHASTIC (unused otherwise): the same seed gives the same bits at the same place, so
+ *          take another one for every matrix and every step (in a captured graph: bnn_quantize_mx4_step).  Element (r, c) takes
  *          h = mix(mix(key + r) + c), key = mix(mix(seed % 2^32) + seed / 2^32), its lower 16 bits for Q and its upper 16 for QT
  *          (mix: x ^= x >> 16, x *= 0x6A09E667, x ^= x >> 15, x *= 0xBB67AE85, x ^= x >> 16, in 32 bits)
  * A block's scale byte is the smallest with all its numbers within 6 times the scale (nothing is cut off, so that stochastic rounding
  * has no bias); a block with an Inf or a NaN gets 255 and codes of 0. */
 int bnn_quantize_mx4(const float* X, int64_t R, int64_t C, int rounding, uint64_t seed, void* Q, void* QT, void* stream);
 
-/* The numbers that a matrix [R][K] of that format holds, exactly (but for those below 2^-126 in size, which fp32 has no more bits for): X out, fp32 [R][K]. */
+/* The same, stochastically, with seed + *step_at for the seed (modulo 2^64), read when the call's work runs: what a captured graph replays takes other bits
+ * at every step.   step_at DEVICE, int64, 8-byte aligned, apart from Q and QT. */
+int bnn_quantize_mx4_step(const float* X, int64_t R, int64_t C, uint64_t seed, const int64_t* step_at, void* Q, void* QT, void* stream);
+
+/* The numbers that a matrix [R][K] of that format holds: X out, fp32 [R][K].  Exact, but for numbers beyond fp32's range, which are infinite
+ * (scale bytes 253 and 254; bnn_quantize_mx4 makes none). */
 int bnn_dequantize_mx4(const void* Q, int64_t R, int64_t K, float* X, void* stream);
 
 /* One layer of 4-bit weights on 4-bit inputs: h^[m][n] = sum_k x[m][k] w[n][k] + bias[n], then the activation.  The sum is taken
@@ -520,8 +526,9 @@ typedef struct bnn_adamw_params {
     int32_t state_bits;     /* 32 or 8                                                                               */
     int32_t reserved;
     uint64_t seed;          /* state_bits 8: of the random bits; another one for every step                         */
-    const float* lr_at;     /* DEVICE, nullable: the learning rate is read there when the update runs               */
-    const int64_t* step_at; /* DEVICE, nullable: so is the step's number (below 1 counts as 1)                      */
+    const float* lr_at;     /* DEVICE, nullable: the learning rate is read there when the update runs, instead of lr  */
+    const int64_t* step_at; /* DEVICE, nullable: so is the step's number, instead of step (below 1 counts as 1), and
+                               seed + step is taken for the seed                                                     */
 } bnn_adamw_params;
 
 /* One update of every tensor.  With t the step, in fp32 with every operation rounded:
@@ -533,6 +540,7 @@ typedef struct bnn_adamw_params {
  * beta2 near 1, which moves v by less than half a code per step, still moves it.  The w of a step comes from m and v before that rounding.
  * u comes from h = mix(mix(key_i + j / 32) + j % 32) for element j of the i-th tensor with elements of the list, from 0,
  * key_i = mix(mix(mix(seed % 2^32) + seed / 2^32) + i), mix as for bnn_quantize_mx4: its lower 16 bits for m, its upper 16 for v.
+ * (the factors' values must be finite, BNN_EINVAL; not checked with lr_at or step_at).
  * An Inf or NaN in a gradient makes the element's w and states NaN or Inf, with 8 bits the states of its block NaN.
  *   tensors  HOST array of n_tensors.  What a launch writes must overlap nothing else it reads or writes (BNN_EINVAL). */
 int bnn_update_adamw(const bnn_adamw_tensor* tensors, int n_tensors, const bnn_adamw_params* params, void* stream);

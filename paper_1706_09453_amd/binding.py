@@ -97,6 +97,7 @@ _SIGNATURES = {
     "bnn_forward": (c_int, [c_void_p, c_int, c_void_p, c_int64, c_void_p, c_void_p, c_size_t, c_void_p]),
     "bnn_mx4_bytes": (c_size_t, [c_int64, c_int64]),
     "bnn_quantize_mx4": (c_int, [c_void_p, c_int64, c_int64, c_int, c_uint64, c_void_p, c_void_p, c_void_p]),
+    "bnn_quantize_mx4_step": (c_int, [c_void_p, c_int64, c_int64, c_uint64, c_void_p, c_void_p, c_void_p, c_void_p]),
     "bnn_dequantize_mx4": (c_int, [c_void_p, c_int64, c_int64, c_void_p, c_void_p]),
     "bnn_layer_mx4": (c_int, [c_void_p, c_void_p, c_void_p, c_int64, c_int64, c_int64, c_int, c_int, c_void_p, c_void_p]),
     "bnn_layer_mx4_realx_workspace_bytes": (c_size_t, [c_int64, c_int64, c_int64]),
@@ -261,6 +262,10 @@ def bnn_mx4_bytes(R: int, K: int) -> int:
 
 def bnn_quantize_mx4(X: int, R: int, C: int, rounding: int, seed: int, Q: int, QT: int, stream: int = 0) -> int:
     return _check(_lib.bnn_quantize_mx4(X, R, C, rounding, seed, Q or None, QT or None, stream or None))
+
+
+def bnn_quantize_mx4_step(X: int, R: int, C: int, seed: int, step_at: int, Q: int, QT: int, stream: int = 0) -> int:
+    return _check(_lib.bnn_quantize_mx4_step(X, R, C, seed, step_at, Q or None, QT or None, stream or None))
 
 
 def bnn_dequantize_mx4(Q: int, R: int, K: int, X: int, stream: int = 0) -> int:

@@ -98,9 +98,12 @@ BNN_EXPORT int bnn_update_adamw(const bnn_adamw_tensor* tensors, int n_tensors, 
 
     // The tensors of one launch are updated side by side: what it writes must lie apart.  Checked for every launch before the first.
     const bool on_device = p.lr_at || p.step_at;
-    const AdamwParams kp{p.lr, p.beta1, p.beta2, p.eps, p.weight_decay, p.step, p.lr_at, p.step_at};
-    const AdamwFactors kf = on_device ? AdamwFactors{} : adamw_factors(p.lr, p.beta1, p.beta2, p.eps, p.weight_decay, p.step);
-    const uint32_t key = seed_key(p.seed);
+    AdamwHost host{};
+    const AdamwDevice device{p.lr, p.beta1, p.beta2, p.eps, p.weight_decay, p.step, p.seed, p.lr_at, p.step_at};
+    if (!on_device) {
+        host = {adamw_factors(p.lr, p.beta1, p.beta2, p.eps, p.weight_decay, p.step), seed_key(p.seed)};
+        if (!std::isfinite(host.f.decay) || !std::isfinite(host.f.size) || !std::isfinite(host.f.q)) return BNN_EINVAL;
+    }
     const bool past = past_caches(tensors, n_tensors);
     for (int pass = 0; pass < 2; ++pass) {
         for (int next = 0, at = 0; next < n_tensors;) {
@@ -126,8 +129,8 @@ BNN_EXPORT int bnn_update_adamw(const bnn_adamw_tensor* tensors, int n_tensors, 
             auto go = [&](auto bits, auto past) {
                 constexpr int B = decltype(bits)::value;
                 constexpr bool P = decltype(past)::value;
-                if (on_device) adamw_kernel<B, P, AdamwParams><<<(unsigned)chunks, 256, 0, st>>>(kp, key, table);
-                else adamw_kernel<B, P, AdamwFactors><<<(unsigned)chunks, 256, 0, st>>>(kf, key, table);
+                if (on_device) adamw_kernel<B, P, AdamwDevice><<<(unsigned)chunks, 256, 0, st>>>(device, table);
+                else adamw_kernel<B, P, AdamwHost><<<(unsigned)chunks, 256, 0, st>>>(host, table);
             };
             using I32 = std::integral_constant<int, 32>;
             using I8 = std::integral_constant<int, 8>;

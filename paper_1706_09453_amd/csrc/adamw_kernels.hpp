@@ -1,4 +1,10 @@
 // AdamW (decoupled weight decay) over many tensors in one launch, states in 32 bits or in 8.
+//
+// 8 bits: blocks of 32 share a power of two.  m is held as signed whole numbers up to 127 of it, v as its root, in whole numbers up to 255, both rounded
+// stochastically.  With beta2 = 0.999 a step moves sqrt(v) by 0.05 % where the gradient vanishes, an eighth of a code or less, which rounding to the nearest would lose for
+// good.  The random step adds up to (2^(e - 127))^2 / 4 to v on average, which decays like everything else in it: sqrt(v) settles no lower than about 5 % of
+// the block's largest, so that steps of elements far below it come out too small, never too large.  (Numbers of 8 bits with an exponent
+// have steps of 6 to 12 % everywhere: rounded stochastically they would add more to v each step than beta2 takes away.)
 #pragma once
 
 #include <type_traits>
@@ -39,19 +45,27 @@ __host__ __device__ inline AdamwFactors adamw_factors(double lr, double beta1, d
     return {(float)beta1, (float)(1.0 - beta1), (float)beta2, (float)(1.0 - beta2), (float)eps, (float)(lr * weight_decay),
             (float)(lr / (1.0 - power(beta1, step))), (float)(1.0 / sqrt(1.0 - power(beta2, step)))};
 }
-// Hyperparameters of a call that has some of them on the device: the factors are then made by every workgroup.
-struct AdamwParams {
+// Hyperparameters of a call, and the key of its random bits: as factors, or where some of them are on the device, as they are; every workgroup
+// then makes the factors, and a step's number that is on the device is added to the seed.
+struct AdamwHost {
+    AdamwFactors f;
+    uint32_t k;
+    __device__ __forceinline__ AdamwFactors factors() const { return f; }
+    __device__ __forceinline__ uint32_t key() const { return k; }
+};
+struct AdamwDevice {
     double lr, beta1, beta2, eps, weight_decay;
-    int64_t step;
+    int64_t t;
+    uint64_t seed;
     const float* lr_at;
     const int64_t* step_at;
-    __device__ AdamwFactors factors() const {
-        const int64_t t = step_at ? *step_at : step;
-        return adamw_factors(lr_at ? (double)*lr_at : lr, beta1, beta2, eps, weight_decay, t > 1 ? t : 1);
+    __device__ __forceinline__ int64_t step() const {
+        const int64_t n = step_at ? *step_at : t;
+        return n > 1 ? n : 1;
     }
+    __device__ __forceinline__ AdamwFactors factors() const { return adamw_factors(lr_at ? (double)*lr_at : lr, beta1, beta2, eps, weight_decay, step()); }
+    __device__ __forceinline__ uint32_t key() const { return seed_key(seed + (step_at ? (uint64_t)step() : 0)); }
 };
-__device__ __forceinline__ AdamwFactors factors_of(const AdamwFactors& f) { return f; }
-__device__ __forceinline__ AdamwFactors factors_of(const AdamwParams& p) { return p.factors(); }
 
 // The tensor that a chunk belongs to: the last one whose first chunk is not behind it.  (A lane per tensor: the arguments are far from the CUs,
 // and looking them through one by one would wait for them as often.)
@@ -202,14 +216,14 @@ __device__ __forceinline__ void adamw_chunk(const AdamwTensor& t, const AdamwFac
     }
 }
 
-// HYPER: AdamwFactors, or AdamwParams where some of them are read on the device.
+// HYPER: AdamwHost or AdamwDevice.
 template <int BITS, bool PAST, class HYPER>
-__global__ __launch_bounds__(256) void adamw_kernel(const HYPER hyper, uint32_t seed, const AdamwTable table) {
+__global__ __launch_bounds__(256) void adamw_kernel(const HYPER hyper, const AdamwTable table) {
     const int i = adamw_tensor_of(table, (int)blockIdx.x);
     const AdamwTensor t = table.t[i];
-    const AdamwFactors f = factors_of(hyper);
+    const AdamwFactors f = hyper.factors();
     const int64_t chunk = (int64_t)((int)blockIdx.x - table.first[i]) * kAdamwChunk;
-    const uint32_t key = mix32(seed + (uint32_t)(table.at + i));
+    const uint32_t key = mix32(hyper.key() + (uint32_t)(table.at + i));
     if (t.vec && chunk + kAdamwChunk <= t.count) adamw_chunk<BITS, true, PAST>(t, f, key, chunk);
     else adamw_chunk<BITS, false, PAST>(t, f, key, chunk);
 }

@@ -18,7 +18,7 @@ constexpr int64_t kMx4MaxK = (int64_t)1 << 22;
 bool mx4_dims_ok(int64_t R, int64_t K) { return R > 0 && K > 0 && R <= kMaxDim && K <= kMaxDim; }
 
 template <bool VEC, bool STOCHASTIC>
-void launch_quantize(const float* X, int R, int C, uint32_t key, void* Q, void* QT, hipStream_t st) {
+void launch_quantize(const float* X, int R, int C, const Mx4Key& key, void* Q, void* QT, hipStream_t st) {
     auto grid = [](int64_t n) { return dim3((unsigned)(n < 65536 ? n : 65536)); };
     const int chunks = (C + 127) / 128, tr = (R + 127) / 128, tc = (C + 63) / 64;
     if (!QT) {
@@ -33,9 +33,8 @@ void launch_quantize(const float* X, int R, int C, uint32_t key, void* Q, void* 
         mx4_quantize_columns_kernel<STOCHASTIC, true><<<grid(((int64_t)tr * tc + 7) / 8 * 8), 256, 0, st>>>(X, R, C, key, Q, QT, tr, tc);
     }
 }
-int run_quantize(const float* X, int64_t R, int64_t C, int rounding, uint64_t seed, void* Q, void* QT, hipStream_t st) {
-    const bool vec = C % 4 == 0 && aligned(X, 16), stochastic = rounding == BNN_ROUND_STOCHASTIC;
-    const uint32_t key = seed_key(seed);
+int run_quantize(const float* X, int64_t R, int64_t C, bool stochastic, const Mx4Key& key, void* Q, void* QT, hipStream_t st) {
+    const bool vec = C % 4 == 0 && aligned(X, 16);
     if (vec && stochastic) launch_quantize<true, true>(X, (int)R, (int)C, key, Q, QT, st);
     else if (vec) launch_quantize<true, false>(X, (int)R, (int)C, key, Q, QT, st);
     else if (stochastic) launch_quantize<false, true>(X, (int)R, (int)C, key, Q, QT, st);
@@ -102,13 +101,24 @@ int run_layer(const void* Xq, const void* Wq, const float* bias, int64_t M, int6
     // Outputs that the caches will not hold, in rows of whole lines, are stored past them: 16384 x 4096 x 4096 190 -> 172 us, 4096 x 2048 x 2048
     // 16.4 -> 15.4.  (Rows that are no whole lines would leave as pieces of lines: 4096 x 2048 x 3400 25 -> 39 us.)
     const int nt = act != BNN_ACT_LOGSOFTMAX && N % 32 == 0 && aligned(Y, 128) && M * N >= (int64_t)8 << 20;
+    // The tile: the smallest of which no more than one (128 x 128 on: two) comes to each CU, since a workgroup's time per stage of K hardly depends on the
+    // tile while it has the CU for itself; with more of them the largest, which moves the least per product, as long as it does not take much more than the
+    // outputs there are.  us with tiles of 64 x 64, 128 x 64, 128 x 128, 256 x 128, 256 x 256:  333 x 1024 x 3400 5.1, 5.2, 5.8, 8.0, 11.4;
+    // 1024 x 2048 x 2048 8.6, 7.9, 9.0, 12, 17;  2048 x 2048 x 2048 13.2, 12.3, 11.0, 13.7, 18.5;  4096 x 2048 x 3400 39, 31, 26.7, 25.0, 26.5;
+    // 8192 x 4096 x 3400 144, 117, 96, 91, 84.
+    struct { int rows, cols, most; } const kTiles[] = {{64, 64, 256}, {128, 64, 256}, {128, 128, 512}, {256, 128, 512}, {256, 256, 0}};
+    int tile = 0;
+    for (; tile < 4 && tiles(kTiles[tile].rows, kTiles[tile].cols) > kTiles[tile].most; ++tile) {
+        auto area = [&](int t) { return tiles(kTiles[t].rows, kTiles[t].cols) * kTiles[t].rows * kTiles[t].cols; };
+        if (4 * area(tile + 1) > 5 * area(tile)) break;
+    }
     bool ok = true;
     auto go = [&](auto a) {
         constexpr int A = decltype(a)::value;
-        if (tiles(64, 64) <= 256) ok = launch_gemm<1, 1, 2, 2, 4, A>(Xq, Wq, bias, (int)M, (int)K, (int)N, Y, yw32, nt, st);
-        else if (tiles(128, 64) <= 256) ok = launch_gemm<2, 1, 2, 2, 4, A>(Xq, Wq, bias, (int)M, (int)K, (int)N, Y, yw32, nt, st);
-        else if (tiles(128, 128) <= 512) ok = launch_gemm<2, 2, 2, 2, 3, A>(Xq, Wq, bias, (int)M, (int)K, (int)N, Y, yw32, nt, st);
-        else if (tiles(256, 128) <= 512) ok = launch_gemm<4, 2, 2, 2, 3, A>(Xq, Wq, bias, (int)M, (int)K, (int)N, Y, yw32, nt, st);
+        if (tile == 0) ok = launch_gemm<1, 1, 2, 2, 4, A>(Xq, Wq, bias, (int)M, (int)K, (int)N, Y, yw32, nt, st);
+        else if (tile == 1) ok = launch_gemm<2, 1, 2, 2, 4, A>(Xq, Wq, bias, (int)M, (int)K, (int)N, Y, yw32, nt, st);
+        else if (tile == 2) ok = launch_gemm<2, 2, 2, 2, 3, A>(Xq, Wq, bias, (int)M, (int)K, (int)N, Y, yw32, nt, st);
+        else if (tile == 3) ok = launch_gemm<4, 2, 2, 2, 3, A>(Xq, Wq, bias, (int)M, (int)K, (int)N, Y, yw32, nt, st);
         else ok = launch_gemm<4, 2, 2, 4, 4, A>(Xq, Wq, bias, (int)M, (int)K, (int)N, Y, yw32, nt, st);
     };
     if (few_frames(M, K)) go_few<false>(Xq, Wq, bias, M, K, N, act, Y, yw32, false, st);
@@ -136,15 +146,29 @@ int check_layer(const void* X, bool real, const void* Wq, const float* bias, int
 
 BNN_EXPORT size_t bnn_mx4_bytes(int64_t R, int64_t K) { return mx4_dims_ok(R, K) ? mx4_bytes(R, K) : 0; }
 
-BNN_EXPORT int bnn_quantize_mx4(const float* X, int64_t R, int64_t C, int rounding, uint64_t seed, void* Q, void* QT, void* stream) {
+static int check_quantize(const float* X, int64_t R, int64_t C, const void* Q, const void* QT) {
     if (R < 0 || C <= 0 || R > kMaxDim || C > kMaxDim) return BNN_ESHAPE;
-    if (rounding != BNN_ROUND_NEAREST && rounding != BNN_ROUND_STOCHASTIC) return BNN_EINVAL;
     if (R == 0) return BNN_OK;
     if (!X || (!Q && !QT)) return BNN_EINVAL;
     if (!aligned(X, 4) || !aligned(Q, 16) || !aligned(QT, 16)) return BNN_EALIGN;
     const size_t xb = (size_t)R * (size_t)C * 4, qb = Q ? mx4_bytes(R, C) : 0, tb = QT ? mx4_bytes(C, R) : 0;
-    if (overlap(X, xb, Q, qb) || overlap(X, xb, QT, tb) || overlap(Q, qb, QT, tb)) return BNN_EINVAL;
-    return run_quantize(X, R, C, rounding, seed, Q, QT, static_cast<hipStream_t>(stream));
+    return overlap(X, xb, Q, qb) || overlap(X, xb, QT, tb) || overlap(Q, qb, QT, tb) ? BNN_EINVAL : BNN_OK;
+}
+
+BNN_EXPORT int bnn_quantize_mx4(const float* X, int64_t R, int64_t C, int rounding, uint64_t seed, void* Q, void* QT, void* stream) {
+    if (rounding != BNN_ROUND_NEAREST && rounding != BNN_ROUND_STOCHASTIC) return BNN_EINVAL;
+    const int rc = check_quantize(X, R, C, Q, QT);
+    if (rc != BNN_OK || R == 0) return rc;
+    return run_quantize(X, R, C, rounding == BNN_ROUND_STOCHASTIC, Mx4Key{seed_key(seed), 0, nullptr}, Q, QT, static_cast<hipStream_t>(stream));
+}
+
+BNN_EXPORT int bnn_quantize_mx4_step(const float* X, int64_t R, int64_t C, uint64_t seed, const int64_t* step_at, void* Q, void* QT, void* stream) {
+    const int rc = check_quantize(X, R, C, Q, QT);
+    if (rc != BNN_OK || R == 0) return rc;
+    if (!step_at) return BNN_EINVAL;
+    if (!aligned(step_at, 8)) return BNN_EALIGN;
+    if ((Q && overlap(step_at, 8, Q, mx4_bytes(R, C))) || (QT && overlap(step_at, 8, QT, mx4_bytes(C, R)))) return BNN_EINVAL;
+    return run_quantize(X, R, C, true, Mx4Key{0, seed, step_at}, Q, QT, static_cast<hipStream_t>(stream));
 }
 
 BNN_EXPORT int bnn_dequantize_mx4(const void* Q, int64_t R, int64_t K, float* X, void* stream) {
@@ -191,6 +215,6 @@ BNN_EXPORT int bnn_layer_mx4_realx(const float* X, const void* Wq, const float* 
         if (act == BNN_ACT_LOGSOFTMAX) launch_log_softmax(static_cast<float*>(Y), (int)M, (int)N, st);
         return launch_status();
     }
-    const int q = run_quantize(X, M, K, BNN_ROUND_NEAREST, 0, workspace, nullptr, st);
+    const int q = run_quantize(X, M, K, false, Mx4Key{}, workspace, nullptr, st);
     return q != BNN_OK ? q : run_layer(workspace, Wq, bias, M, K, N, act, word_bits, Y, st);
 }

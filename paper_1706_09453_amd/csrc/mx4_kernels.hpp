@@ -57,6 +57,14 @@ __device__ __forceinline__ uint32_t mx4_top8(const float (&v)[8]) {
     return t;
 }
 
+// Where a launch's random bits start: a key, or where the step's number is on the device, the seed that it is added to.
+struct Mx4Key {
+    uint32_t key;
+    uint64_t seed;
+    const int64_t* step_at;
+    __device__ __forceinline__ uint32_t get() const { return step_at ? seed_key(seed + (uint64_t)*step_at) : key; }
+};
+
 // 8 numbers of row r from column c on; 0 outside the matrix
 template <bool VEC>
 __device__ __forceinline__ void mx4_load8(const float* __restrict__ X, int R, int C, int r, int c, float (&v)[8]) {
@@ -76,7 +84,8 @@ __device__ __forceinline__ void mx4_load8(const float* __restrict__ X, int R, in
 // 4-bit codes of X [R][C] along its rows, Q [R][C].  Bound by memory: a workgroup takes 16 PASSES rows of a chunk, all of it requested before
 // the first is used; consecutive workgroups go along the row.  Grid: row groups * chunks, the chunks fastest.
 template <bool VEC, bool STOCHASTIC, int PASSES>
-__global__ __launch_bounds__(256) void mx4_quantize_rows_kernel(const float* __restrict__ X, int R, int C, uint32_t key, void* __restrict__ Q, int chunks) {
+__global__ __launch_bounds__(256) void mx4_quantize_rows_kernel(const float* __restrict__ X, int R, int C, const Mx4Key random, void* __restrict__ Q, int chunks) {
+    const uint32_t key = STOCHASTIC ? random.get() : 0u;
     const int64_t items = (int64_t)((R + 16 * PASSES - 1) / (16 * PASSES)) * chunks;
     unsigned char* codes = static_cast<unsigned char*>(Q);
     unsigned char* scales = reinterpret_cast<unsigned char*>(mx4_scales(Q, R, C));
@@ -114,11 +123,12 @@ __global__ __launch_bounds__(256) void mx4_quantize_rows_kernel(const float* __r
 // L2.  Grid: a multiple of 8.
 constexpr int kMx4TileLd = 64 + 4;   // floats of a row in LDS
 template <bool STOCHASTIC, bool ROWS>
-__global__ __launch_bounds__(256) void mx4_quantize_columns_kernel(const float* __restrict__ X, int R, int C, uint32_t key, void* __restrict__ Q,
+__global__ __launch_bounds__(256) void mx4_quantize_columns_kernel(const float* __restrict__ X, int R, int C, const Mx4Key random, void* __restrict__ Q,
                                                                    void* __restrict__ QT, int tiles_r, int tiles_c) {
     __shared__ __attribute__((aligned(16))) float rows_s[ROWS ? 4 : 1][ROWS ? 32 : 1][kMx4TileLd];
     __shared__ __attribute__((aligned(16))) uint4 codes_s[64][4];
     __shared__ __attribute__((aligned(4))) unsigned char scales_s[64][4];
+    const uint32_t key = STOCHASTIC ? random.get() : 0u;
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = lane_id();
     unsigned char *codes_q = static_cast<unsigned char*>(Q), *codes_t = static_cast<unsigned char*>(QT);
     unsigned char* scales_q = ROWS ? reinterpret_cast<unsigned char*>(mx4_scales(Q, R, C)) : nullptr;

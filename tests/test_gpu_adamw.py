@@ -161,7 +161,8 @@ def test_numbers_out_of_range(G, bnn, bits):
 
 
 def test_hyperparameters_on_the_device_in_a_graph(G, bnn):
-    """A captured update that reads its step and its learning rate from the device, replayed, against eager calls with the same values."""
+    """A captured update that reads its step and its learning rate from the device, replayed, against eager calls with the same values
+    (the step is added to the seed).  A step below 1 counts as 1."""
     for bits in (32, 8):
         rng = np.random.default_rng(bits)
         sizes = [40000, 77]
@@ -178,11 +179,18 @@ def test_hyperparameters_on_the_device_in_a_graph(G, bnn):
             step.fill_(s)
             lr.fill_(np.float32(1e-3) * s)
             graph.replay()
-            bnn.bnn_update_adamw(eager_list, 2, params(bnn, bits, s, 31, lr=float(np.float32(1e-3) * np.float32(s))), G.stream())
+            bnn.bnn_update_adamw(eager_list, 2, params(bnn, bits, s, 31 + s, lr=float(np.float32(1e-3) * np.float32(s))), G.stream())
             torch.cuda.synchronize()
             for t, e, a in zip(ts, es, arrays):
                 for k in a:
                     assert same(t.get(k), e.get(k)), (bits, s, k)
+        step.fill_(-3)
+        graph.replay()
+        bnn.bnn_update_adamw(eager_list, 2, params(bnn, bits, 1, 32, lr=float(lr.item())), G.stream())
+        torch.cuda.synchronize()
+        for t, e, a in zip(ts, es, arrays):
+            for k in a:
+                assert same(t.get(k), e.get(k)), (bits, k)
 
 
 def test_more_than_2_to_32_elements(G, bnn):

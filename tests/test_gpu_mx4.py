@@ -143,6 +143,22 @@ def test_dequantize(G, bnn, R, K):
         assert np.array_equal(x.get(np.float32).reshape(R, K), mx.unpack(buf, R, K).astype(np.float32), equal_nan=True)
 
 
+def test_dequantize_scales_from_the_smallest_to_the_largest(G, bnn):
+    """Every scale byte with every code: exact, and infinite beyond fp32's range."""
+    R, K = 255, 32
+    codes = np.zeros((R, 128), np.int64)
+    codes[:, :32] = np.arange(32) % 16
+    e = np.zeros((R, 4), np.int64)
+    e[:, 0] = np.arange(R)
+    buf = mx.pack(codes, e)
+    q, x = Buffer(buf.size).put(buf), Buffer(R * K * 4)
+    bnn.bnn_dequantize_mx4(q.ptr, R, K, x.ptr, G.stream())
+    want = mx.unpack(buf, R, K)
+    with np.errstate(over="ignore"):
+        assert np.array_equal(x.get(np.float32).reshape(R, K), want.astype(np.float32))
+    assert np.isfinite(want.astype(np.float32)[:253]).all()
+
+
 def random_packed(rng, R, K, e_lo=120, e_hi=130, whole=False):
     """A packed matrix with random codes; whole: values that are multiples of 1/4 up to 12."""
     C = (K + 127) // 128
@@ -165,7 +181,8 @@ def layer(G, bnn, xq, wq, bias, M, K, N, act, wb=32, offset=0):
 
 
 LAYERS = [(1, 1, 1), (1, 32, 1), (2, 33, 5), (3, 440, 70), (5, 129, 33), (15, 512, 64), (16, 2048, 100), (17, 130, 257), (31, 96, 31), (33, 1000, 65), (64, 128, 128),
-          (65, 256, 129), (100, 3000, 40), (127, 384, 255), (129, 127, 300), (200, 640, 513), (257, 2048, 130), (300, 200, 1003), (520, 1100, 260), (1100, 160, 1100)]
+          (65, 256, 129), (100, 3000, 40), (127, 384, 255), (129, 127, 300), (200, 640, 513), (257, 2048, 130), (300, 200, 1003), (520, 1100, 260), (1100, 160, 1100), (3000, 130, 1500), (9000, 128, 1700), (20000, 129, 9), (40, 300, 17000),
+          (20000, 64, 1000), (70000, 40, 7)]
 
 
 @pytest.mark.parametrize("M,K,N", LAYERS)
@@ -261,7 +278,7 @@ def test_layer_from_fp32_frames(G, bnn, M, K, N):
     assert np.array_equal(y.get(np.uint64).reshape(M, yw), orc.pack_sign(want.astype(np.float32), 64))
 
 
-@pytest.mark.parametrize("M,act", [(1, "linear"), (3, "sigmoid"), (16, "hardtanh"), (40, "logsoftmax"), (200, "linear")])
+@pytest.mark.parametrize("M,act", [(1, "linear"), (3, "sigmoid"), (16, "hardtanh"), (40, "logsoftmax"), (200, "linear"), (2, "logsoftmax"), (11, "linear")])
 def test_layer_from_fp32_frames_with_real_sums(G, bnn, M, act):
     K, N = 700, 333
     rng = np.random.default_rng(M)

@@ -65,10 +65,13 @@ class Net:
         self.list = bnn.make_adamw_array(descs)
 
     def seed(self, l, step):
-        return step * 1000 + l
+        return l * (1 << 40) + step
 
-    def quantize(self, X, Q, QT, rounding, seed, st):
+    def quantize(self, X, Q, QT, rounding, seed, st, on_device=False):
         R, C = X.shape
+        if on_device:   # the seed, and the step's number there
+            self.bnn.bnn_quantize_mx4_step(X.data_ptr(), R, C, seed, self.step.data_ptr(), Q.data_ptr(), QT.data_ptr(), st)
+            return
         self.bnn.bnn_quantize_mx4(X.data_ptr(), R, C, rounding, seed, Q.data_ptr(), QT.data_ptr(), st)
 
     def forward(self, st):
@@ -80,14 +83,14 @@ class Net:
             act = b.BNN_ACT_SIGMOID if l + 1 < self.L else b.BNN_ACT_LOGSOFTMAX
             b.bnn_layer_mx4(self.hq[l].data_ptr(), self.Wq[l].data_ptr(), self.b[l].data_ptr(), self.M, k, n, act, 32, self.h[l + 1].data_ptr(), st)
 
-    def backward(self, step, st):
+    def backward(self, step, st, on_device=False):
         b, M = self.bnn, self.M
         b.bnn_softmax_xent_grad(self.h[-1].data_ptr(), self.labels.data_ptr(), M, self.dims[-1], self.g[-1].data_ptr(), st)
         for l in range(self.L - 1, -1, -1):
             n, k = self.W[l].shape
             if l + 1 < self.L:
                 b.bnn_sigmoid_grad(self.gh[l + 1].data_ptr(), self.h[l + 1].data_ptr(), M * n, self.g[l].data_ptr(), st)
-            self.quantize(self.g[l], self.gq[l], self.gqT[l], b.BNN_ROUND_STOCHASTIC, self.seed(l, step), st)
+            self.quantize(self.g[l], self.gq[l], self.gqT[l], b.BNN_ROUND_STOCHASTIC, self.seed(l, step), st, on_device)
             b.bnn_layer_mx4(self.gqT[l].data_ptr(), self.hqT[l].data_ptr(), 0, n, M, k, b.BNN_ACT_LINEAR, 32, self.gw[l].data_ptr(), st)
             b.bnn_bias_grad(self.g[l].data_ptr(), M, n, self.gb[l].data_ptr(), st)
             if l > 0:
@@ -96,7 +99,7 @@ class Net:
     HYPER = dict(lr=1e-2, beta1=0.9, beta2=0.99, eps=1e-8, weight_decay=0.01)
 
     def update(self, step, st, on_device=False):
-        p = self.bnn.bnn_adamw_params(**self.HYPER, step=0 if on_device else step, state_bits=self.bits, seed=7, step_at=self.step.data_ptr() if on_device else 0)
+        p = self.bnn.bnn_adamw_params(**self.HYPER, step=0 if on_device else step, state_bits=self.bits, seed=7 if on_device else 7 + step, step_at=self.step.data_ptr() if on_device else 0)
         self.bnn.bnn_update_adamw(self.list, 2 * self.L, p, st)
 
     def tensors(self):
@@ -147,7 +150,7 @@ def test_steps_of_training(G, bnn, bits, M, dims):
                 want_w, m, v, _ = mx.adamw(a["w"], a["g"], a["m"], a["v"], step, **kw)
                 want = {"m": m, "v": v}
             else:
-                want_w, m, ms, v, vs = mx.adamw8(a["w"], a["g"], a["m"].view(np.int8), a["m_scale"], a["v"], a["v_scale"], step, 7, i, **kw)
+                want_w, m, ms, v, vs = mx.adamw8(a["w"], a["g"], a["m"].view(np.int8), a["m_scale"], a["v"], a["v_scale"], step, 7 + step, i, **kw)
                 want = {"m": m.view(np.uint8), "m_scale": ms, "v": v, "v_scale": vs}
             assert np.array_equal(host(w).reshape(-1), want_w), i
             for k in want:
@@ -163,7 +166,7 @@ def test_a_captured_step_is_the_eager_one(G, bnn):
         torch.cuda.synchronize()
         with torch.cuda.graph(graph, stream=st):
             a.forward(st.cuda_stream)
-            a.backward(0, st.cuda_stream)
+            a.backward(0, st.cuda_stream, on_device=True)
             a.update(0, st.cuda_stream, on_device=True)
         for step in range(1, 5):
             a.step.fill_(step)
@@ -172,7 +175,7 @@ def test_a_captured_step_is_the_eager_one(G, bnn):
             torch.cuda.synchronize()
             graph.replay()
             b.forward(G.stream())
-            b.backward(0, G.stream())
+            b.backward(step, G.stream())
             b.update(step, G.stream())
             torch.cuda.synchronize()
             for x, y in zip(a.tensors(), b.tensors()):

@@ -50,6 +50,12 @@ def test_quantize_refusals(bnn):
     assert _status(fn, P, 4, 64, 0, 0, P - 256 - 16 + 16, 0) == bnn.BNN_EINVAL        # the scale words on X's first bytes
     assert _status(fn, P, 4, 64, 0, 0, Q, Q + 256) == bnn.BNN_EINVAL                  # one form's scales on the other's codes
     assert fn(0, 0, 64, 0, 0, 0, 0) == 0
+    fn = bnn.bnn_quantize_mx4_step
+    assert _status(fn, P, 4, 64, 0, 0, Q, 0) == bnn.BNN_EINVAL and _status(fn, P, 4, 64, 0, S + 4, Q, 0) == bnn.BNN_EALIGN
+    assert _status(fn, P, 4, 64, 0, Q + 8, Q, 0) == bnn.BNN_EINVAL and _status(fn, P, 4, 64, 0, R + 256, 0, R) == bnn.BNN_EINVAL
+    assert _status(fn, 0, 4, 64, 0, S, Q, 0) == bnn.BNN_EINVAL and _status(fn, P, 4, 64, 0, S, 0, 0) == bnn.BNN_EINVAL
+    assert _status(fn, P, -1, 64, 0, S, Q, 0) == bnn.BNN_ESHAPE and _status(fn, P + 2, 4, 64, 0, S, Q, 0) == bnn.BNN_EALIGN
+    assert fn(0, 0, 64, 0, 0, 0, 0) == 0
     fn = bnn.bnn_dequantize_mx4
     assert _status(fn, 0, 4, 64, Q) == bnn.BNN_EINVAL and _status(fn, P, 4, 64, 0) == bnn.BNN_EINVAL
     assert _status(fn, P, -1, 64, Q) == bnn.BNN_ESHAPE and _status(fn, P, 4, 0, Q) == bnn.BNN_ESHAPE
@@ -101,7 +107,7 @@ def test_adamw_refusals(bnn):
     assert st(count=-1) == st(count=(1 << 35) + 1) == bnn.BNN_ESHAPE
     assert st(clip=2) == st(clip=-1) == bnn.BNN_EINVAL
     for bad in (dict(lr=-1e-3), dict(lr=nan), dict(lr=inf), dict(lr=1e39), dict(beta1=1.0), dict(beta1=-0.1), dict(beta2=1.0), dict(beta2=nan), dict(eps=0.0),
-                dict(eps=1e-50), dict(eps=nan), dict(eps=inf), dict(weight_decay=-1.0), dict(weight_decay=nan), dict(step=0), dict(step=-5), dict(state_bits=16),
+                dict(eps=1e-50), dict(eps=nan), dict(eps=inf), dict(weight_decay=-1.0), dict(weight_decay=nan), dict(step=0), dict(step=-5), dict(lr=1e30, weight_decay=1e30), dict(lr=1e38, beta1=0.9999), dict(state_bits=16),
                 dict(state_bits=0)):
         assert st(_params(bnn, **bad)) == bnn.BNN_EINVAL, bad
     assert st(_params(bnn, lr_at=P + 2)) == st(_params(bnn, step_at=P + 4)) == bnn.BNN_EALIGN
