@@ -178,11 +178,20 @@ BNN_EXPORT int bnn_dequantize_mx4(const void* Q, int64_t R, int64_t K, float* X,
     if (!aligned(Q, 16) || !aligned(X, 4)) return BNN_EALIGN;
     if (overlap(Q, mx4_bytes(R, K), X, (size_t)R * (size_t)K * 4)) return BNN_EINVAL;
     const int chunks = (int)mx4_chunks(K);
-    const int64_t blocks = (R * chunks * 32 + 255) / 256;
-    const unsigned grid = (unsigned)(blocks < 65536 ? blocks : 65536);
     hipStream_t st = static_cast<hipStream_t>(stream);
-    if (K % 4 == 0 && aligned(X, 16)) mx4_dequantize_kernel<true><<<grid, 256, 0, st>>>(Q, (int)R, (int)K, chunks, X);
-    else mx4_dequantize_kernel<false><<<grid, 256, 0, st>>>(Q, (int)R, (int)K, chunks, X);
+    auto go = [&](auto vec, auto passes) {
+        constexpr int P = decltype(passes)::value;
+        const int64_t groups = ((R + 8 * P - 1) / (8 * P)) * chunks;
+        mx4_dequantize_kernel<decltype(vec)::value, P><<<(unsigned)(groups < 65536 ? groups : 65536), 256, 0, st>>>(Q, (int)R, (int)K, chunks, X);
+    };
+    using I1 = std::integral_constant<int, 1>;
+    using I2 = std::integral_constant<int, 2>;
+    // 8 rows a workgroup while that leaves CUs idle, 16 beyond
+    const bool vec = K % 4 == 0 && aligned(X, 16), small = ((R + 15) / 16) * chunks < 512;
+    if (vec && small) go(std::true_type{}, I1{});
+    else if (vec) go(std::true_type{}, I2{});
+    else if (small) go(std::false_type{}, I1{});
+    else go(std::false_type{}, I2{});
     return launch_status();
 }
 

@@ -82,7 +82,8 @@ __device__ __forceinline__ void mx4_load8(const float* __restrict__ X, int R, in
 }
 
 // 4-bit codes of X [R][C] along its rows, Q [R][C].  Bound by memory: a workgroup takes 16 PASSES rows of a chunk, all of it requested before
-// the first is used; consecutive workgroups go along the row.  Grid: row groups * chunks, the chunks fastest.
+// the first is used; consecutive workgroups go along the row.  Rows that are not 16-byte aligned go through LDS, so that a wave reads a row in
+// one piece (1003 x 3411 10.1 us with every lane reading its own 8 numbers, 5.3 so).  Grid: row groups * chunks, the chunks fastest.
 template <bool VEC, bool STOCHASTIC, int PASSES>
 __global__ __launch_bounds__(256) void mx4_quantize_rows_kernel(const float* __restrict__ X, int R, int C, const Mx4Key random, void* __restrict__ Q, int chunks) {
     const uint32_t key = STOCHASTIC ? random.get() : 0u;
@@ -94,8 +95,34 @@ __global__ __launch_bounds__(256) void mx4_quantize_rows_kernel(const float* __r
         const int64_t group = i / chunks;
         const int chunk = (int)(i - group * chunks), r0 = (int)group * (16 * PASSES) + ((int)threadIdx.x >> 4), c = chunk * kMx4Chunk + 8 * sub;
         float v[PASSES][8];
+        if constexpr (VEC) {
 #pragma unroll
-        for (int p = 0; p < PASSES; ++p) mx4_load8<VEC>(X, R, C, r0 + 16 * p, c, v[p]);
+            for (int p = 0; p < PASSES; ++p) mx4_load8<true>(X, R, C, r0 + 16 * p, c, v[p]);
+        } else {
+            __shared__ __attribute__((aligned(16))) float rows_s[16 * PASSES][kMx4Chunk];
+            const int wave = (int)threadIdx.x >> 6, lane = lane_id(), first = (int)group * (16 * PASSES);
+            float x[4 * PASSES][2];
+#pragma unroll
+            for (int j = 0; j < 4 * PASSES; ++j)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int r = first + 4 * j + wave, k = chunk * kMx4Chunk + 64 * h + lane;
+                    x[j][h] = r < R && k < C ? X[(size_t)r * C + k] : 0.0f;
+                }
+            __syncthreads();   // (the rows before have been read)
+#pragma unroll
+            for (int j = 0; j < 4 * PASSES; ++j)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) rows_s[4 * j + wave][64 * h + lane] = x[j][h];
+            __syncthreads();
+#pragma unroll
+            for (int p = 0; p < PASSES; ++p) {
+                const float4* s = reinterpret_cast<const float4*>(&rows_s[((int)threadIdx.x >> 4) + 16 * p][8 * sub]);
+                const float4 lo = s[0], hi = s[1];
+                v[p][0] = lo.x; v[p][1] = lo.y; v[p][2] = lo.z; v[p][3] = lo.w;
+                v[p][4] = hi.x; v[p][5] = hi.y; v[p][6] = hi.z; v[p][7] = hi.w;
+            }
+        }
 #pragma unroll
         for (int p = 0; p < PASSES; ++p) {
             const int r = r0 + 16 * p;
@@ -200,27 +227,48 @@ __global__ __launch_bounds__(256) void mx4_quantize_columns_kernel(const float* 
     }
 }
 
-// The values that the codes of a matrix [R][K] stand for, fp32.  A lane takes 4 elements.
-template <bool VEC>
+// The values that the codes of a matrix [R][K] stand for, fp32.  Bound by memory: 32 lanes take a row's chunk, 4 numbers each, side by side where rows
+// are 16-byte aligned (VEC) and 32 apart otherwise, so that either stores whole lines; a workgroup takes 8 PASSES rows of a chunk.  Grid: row groups * chunks, the chunks fastest.
+template <bool VEC, int PASSES>
 __global__ __launch_bounds__(256) void mx4_dequantize_kernel(const void* __restrict__ Q, int R, int K, int chunks, float* __restrict__ X) {
+    const int64_t items = (int64_t)((R + 8 * PASSES - 1) / (8 * PASSES)) * chunks;
     const unsigned char* codes = static_cast<const unsigned char*>(Q);
-    const unsigned char* scales = reinterpret_cast<const unsigned char*>(mx4_scales(Q, R, K));
-    const int64_t quads = (int64_t)R * chunks * 32, stride = (int64_t)gridDim.x * 256;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < quads; i += stride) {
-        const int64_t rc = i >> 5;
-        const int r = (int)(rc / chunks), chunk = (int)(rc - (int64_t)r * chunks), sub = (int)(i & 31), k = chunk * 128 + 4 * sub;
-        if (k >= K) continue;
-        const uint32_t c = *reinterpret_cast<const uint16_t*>(codes + 2 * i);
-        const float s = __uint_as_float((uint32_t)scales[((size_t)chunk * R + r) * 4 + (sub >> 3)] << 23);   // (the instruction takes the field: 0 is 2^-127, 255 NaN)
-        const f32x2 lo = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, s, 0), hi = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, s, 1);
-        const float v[4] = {lo.x, lo.y, hi.x, hi.y};
-        float* p = X + (size_t)r * K + k;
-        if (VEC && k + 4 <= K) {
-            *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
-        } else {
+    const uint32_t* scales = mx4_scales(Q, R, K);
+    const int sub = (int)threadIdx.x & 31;
+    for (int64_t i = blockIdx.x; i < items; i += gridDim.x) {
+        const int64_t group = i / chunks;
+        const int chunk = (int)(i - group * chunks), r0 = (int)group * (8 * PASSES) + ((int)threadIdx.x >> 5);
+        uint32_t c[PASSES][4], e[PASSES];
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-                if (k + j < K) p[j] = v[j];
+        for (int p = 0; p < PASSES; ++p) {
+            const int r = min(r0 + 8 * p, R - 1);
+            const unsigned char* row = codes + ((size_t)r * chunks + chunk) * kMx4ChunkBytes;
+            e[p] = scales[(size_t)chunk * R + r];
+            if constexpr (VEC) {
+                c[p][0] = *reinterpret_cast<const uint16_t*>(row + 2 * sub);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) c[p][j] = row[16 * j + (sub >> 1)];
+            }
+        }
+#pragma unroll
+        for (int p = 0; p < PASSES; ++p) {
+            const int r = r0 + 8 * p;
+            if (r >= R) continue;
+            // (the conversion takes the field of the scale's exponent: 0 is 2^-127, 255 NaN)
+            if constexpr (VEC) {
+                const int k = chunk * kMx4Chunk + 4 * sub;
+                const float s = __uint_as_float(((e[p] >> (sub & 24)) & 0xFFu) << 23);
+                const f32x2 lo = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c[p][0], s, 0), hi = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c[p][0], s, 1);
+                if (k < K) *reinterpret_cast<float4*>(X + (size_t)r * K + k) = make_float4(lo.x, lo.y, hi.x, hi.y);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int k = chunk * kMx4Chunk + 32 * j + sub;
+                    const f32x2 v = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c[p][j], __uint_as_float(((e[p] >> (8 * j)) & 0xFFu) << 23), 0);
+                    if (k < K) X[(size_t)r * K + k] = sub & 1 ? v.y : v.x;
+                }
+            }
         }
     }
 }
