@@ -144,15 +144,18 @@ __global__ __launch_bounds__(256) void mx4_quantize_rows_kernel(const float* __r
 
 // Along its columns, QT [C][R], and with ROWS along its rows too.  A workgroup takes 128 rows (a chunk of the columns form) of 64 columns.  For the
 // columns form a lane holds 32 rows of a column, a block; what it writes is collected in LDS, so that it leaves as 64 bytes per column and whole
-// lines of scale words.  For the rows form the wave's numbers go through LDS: 8 lanes a row, 8 numbers each.  (Their random bits are mixed once
-// more: handed on through LDS as well, they cost more in workgroups per CU than they save, 16384 x 4096 120 us against 96.)
+// lines of scale words.  For the rows form the wave's numbers go through LDS, 8 lanes a row, 8 numbers each, and then the lower halves of their random
+// bits through the same place (beside the numbers they would cost more in workgroups per CU than mixing them once more).
 // Workgroups go round the eight XCDs: each takes a run of consecutive tiles, so that the pieces of a line that several of them write meet in one
 // L2.  Grid: a multiple of 8.
-constexpr int kMx4TileLd = 64 + 4;   // floats of a row in LDS
+union __attribute__((aligned(16))) Mx4Tile32 {   // 32 rows of 64 numbers in LDS, and a pad
+    float numbers[32][64 + 4];
+    uint16_t bits[32][64 + 8];
+};
 template <bool STOCHASTIC, bool ROWS>
-__global__ __launch_bounds__(256) void mx4_quantize_columns_kernel(const float* __restrict__ X, int R, int C, const Mx4Key random, void* __restrict__ Q,
+__global__ __launch_bounds__(256, 4) void mx4_quantize_columns_kernel(const float* __restrict__ X, int R, int C, const Mx4Key random, void* __restrict__ Q,
                                                                    void* __restrict__ QT, int tiles_r, int tiles_c) {
-    __shared__ __attribute__((aligned(16))) float rows_s[ROWS ? 4 : 1][ROWS ? 32 : 1][kMx4TileLd];
+    __shared__ Mx4Tile32 tile_s[ROWS ? 4 : 1];
     __shared__ __attribute__((aligned(16))) uint4 codes_s[64][4];
     __shared__ __attribute__((aligned(4))) unsigned char scales_s[64][4];
     const uint32_t key = STOCHASTIC ? random.get() : 0u;
@@ -161,19 +164,30 @@ __global__ __launch_bounds__(256) void mx4_quantize_columns_kernel(const float* 
     unsigned char* scales_q = ROWS ? reinterpret_cast<unsigned char*>(mx4_scales(Q, R, C)) : nullptr;
     uint32_t* scales_t = mx4_scales(QT, C, R);
     const int chunks_q = (C + 127) / 128;
+    Mx4Tile32& tile = tile_s[ROWS ? wave : 0];
     const int64_t total = (int64_t)tiles_r * tiles_c, per_xcd = (total + 7) >> 3;
     for (int64_t k = blockIdx.x >> 3; k < per_xcd; k += gridDim.x >> 3) {
         const int64_t t = (blockIdx.x & 7) * per_xcd + k;
         if (t >= total) break;
         const int tr = (int)(t / tiles_c), tc = (int)(t - (int64_t)tr * tiles_c), c0 = tc * 64, r0 = tr * 128, rb = r0 + 32 * wave;
+        float x[4][8];   // the lane's numbers of the rows form
         {
             const int c = c0 + lane;
             float v[32];
 #pragma unroll
             for (int j = 0; j < 32; ++j) v[j] = rb + j < R && c < C ? X[(size_t)(rb + j) * C + c] : 0.0f;
-            if constexpr (ROWS) {
+            if constexpr (ROWS) {   // (a wave's own part of LDS: first the numbers, then their bits)
 #pragma unroll
-                for (int j = 0; j < 32; ++j) rows_s[wave][j][lane] = v[j];
+                for (int j = 0; j < 32; ++j) tile.numbers[j][lane] = v[j];
+                asm volatile("" ::: "memory");
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float4* s = reinterpret_cast<const float4*>(&tile.numbers[8 * i + (lane >> 3)][8 * (lane & 7)]);
+                    const float4 lo = s[0], hi = s[1];
+                    x[i][0] = lo.x; x[i][1] = lo.y; x[i][2] = lo.z; x[i][3] = lo.w;
+                    x[i][4] = hi.x; x[i][5] = hi.y; x[i][6] = hi.z; x[i][7] = hi.w;
+                }
+                asm volatile("" ::: "memory");
             }
             uint32_t top = 0;
 #pragma unroll
@@ -182,10 +196,14 @@ __global__ __launch_bounds__(256) void mx4_quantize_columns_kernel(const float* 
             uint32_t w[4];
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                const float x[8] = {v[8 * q], v[8 * q + 1], v[8 * q + 2], v[8 * q + 3], v[8 * q + 4], v[8 * q + 5], v[8 * q + 6], v[8 * q + 7]};
+                const float y[8] = {v[8 * q], v[8 * q + 1], v[8 * q + 2], v[8 * q + 3], v[8 * q + 4], v[8 * q + 5], v[8 * q + 6], v[8 * q + 7]};
                 if constexpr (STOCHASTIC)
-                    w[q] = mx4_stochastic8(x, e, [&](int j) { return mix32(mix32(key + (uint32_t)(rb + 8 * q + j)) + (uint32_t)c) >> 16; });
-                else w[q] = mx4_nearest8(x, e);
+                    w[q] = mx4_stochastic8(y, e, [&](int j) {
+                        const uint32_t h = mix32(mix32(key + (uint32_t)(rb + 8 * q + j)) + (uint32_t)c);
+                        if constexpr (ROWS) tile.bits[8 * q + j][lane] = (uint16_t)h;
+                        return h >> 16;
+                    });
+                else w[q] = mx4_nearest8(y, e);
             }
             codes_s[lane][wave] = make_uint4(w[0], w[1], w[2], w[3]);
             scales_s[lane][wave] = (unsigned char)e;
@@ -201,15 +219,14 @@ __global__ __launch_bounds__(256) void mx4_quantize_columns_kernel(const float* 
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int j = 8 * i + (lane >> 3), r = rb + j;
-                const float4 lo = *reinterpret_cast<const float4*>(&rows_s[wave][j][8 * sub]), hi = *reinterpret_cast<const float4*>(&rows_s[wave][j][8 * sub + 4]);
-                const float v[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
-                const uint32_t e = mx_scale<MxE2M1>(max_of_4_lanes(mx4_top8(v)));
+                const uint32_t e = mx_scale<MxE2M1>(max_of_4_lanes(mx4_top8(x[i])));
                 uint32_t w;
                 if constexpr (STOCHASTIC) {
-                    const uint32_t row_key = mix32(key + (uint32_t)r);
-                    w = mx4_stochastic8(v, e, [&](int n) { return mix32(row_key + (uint32_t)(c0 + 8 * sub + n)) & 0xFFFFu; });
+                    const uint4 h = *reinterpret_cast<const uint4*>(&tile.bits[j][8 * sub]);
+                    const uint32_t pair[4] = {h.x, h.y, h.z, h.w};
+                    w = mx4_stochastic8(x[i], e, [&](int n) { return n & 1 ? pair[n >> 1] >> 16 : pair[n >> 1] & 0xFFFFu; });
                 } else {
-                    w = mx4_nearest8(v, e);
+                    w = mx4_nearest8(x[i], e);
                 }
                 if (r < R) {
                     const size_t chunk = (size_t)r * chunks_q + (tc >> 1);
