@@ -13,7 +13,7 @@ namespace {
 
 using namespace bnn;
 
-constexpr int64_t kMaxCount = (int64_t)1 << 35;   // 2^23 workgroups; blocks of 32 are counted in 32 bits
+constexpr int64_t kMaxCount = (int64_t)1 << 35;   // 2^25 workgroups; blocks of 32 are counted in 32 bits
 
 struct Range {
     uintptr_t from, to;
@@ -57,12 +57,9 @@ int64_t fill(AdamwTable& table, const bnn_adamw_tensor* tensors, int n, int& nex
     return chunks;
 }
 
-// Tensors whose arrays the last level of cache (256 MB) does not hold beside each other are read and written past the caches: 29 million elements
-// 157 -> 141 us, with 8-bit states 107 -> 88, reading those back 51 -> 43; 1.3 million 8.9 and 9.6.
-bool past_caches(const bnn_adamw_tensor* tensors, int n) {
-    int64_t elements = 0;
-    for (int i = 0; i < n; ++i) elements += tensors[i].count;
-    return elements >= (int64_t)8 << 20;
+dim3 grid_of(int64_t chunks) {
+    const int64_t x = std::min(chunks, (int64_t)1 << 23);
+    return dim3((unsigned)x, (unsigned)((chunks + x - 1) / x));
 }
 
 int ranges_of(const bnn_adamw_tensor& t, int bits, Range* r) {
@@ -104,7 +101,6 @@ BNN_EXPORT int bnn_update_adamw(const bnn_adamw_tensor* tensors, int n_tensors, 
         host = {adamw_factors(p.lr, p.beta1, p.beta2, p.eps, p.weight_decay, p.step), seed_key(p.seed)};
         if (!std::isfinite(host.f.decay) || !std::isfinite(host.f.size) || !std::isfinite(host.f.q)) return BNN_EINVAL;
     }
-    const bool past = past_caches(tensors, n_tensors);
     for (int pass = 0; pass < 2; ++pass) {
         for (int next = 0, at = 0; next < n_tensors;) {
             AdamwTable table;
@@ -126,18 +122,13 @@ BNN_EXPORT int bnn_update_adamw(const bnn_adamw_tensor* tensors, int n_tensors, 
                 continue;
             }
             hipStream_t st = static_cast<hipStream_t>(stream);
-            auto go = [&](auto bits, auto past) {
+            auto go = [&](auto bits) {
                 constexpr int B = decltype(bits)::value;
-                constexpr bool P = decltype(past)::value;
-                if (on_device) adamw_kernel<B, P, AdamwDevice><<<(unsigned)chunks, 256, 0, st>>>(device, table);
-                else adamw_kernel<B, P, AdamwHost><<<(unsigned)chunks, 256, 0, st>>>(host, table);
+                if (on_device) adamw_kernel<B, AdamwDevice><<<grid_of(chunks), 256, 0, st>>>(device, table);
+                else adamw_kernel<B, AdamwHost><<<grid_of(chunks), 256, 0, st>>>(host, table);
             };
-            using I32 = std::integral_constant<int, 32>;
-            using I8 = std::integral_constant<int, 8>;
-            if (p.state_bits == 32 && past) go(I32{}, std::true_type{});
-            else if (p.state_bits == 32) go(I32{}, std::false_type{});
-            else if (past) go(I8{}, std::true_type{});
-            else go(I8{}, std::false_type{});
+            if (p.state_bits == 32) go(std::integral_constant<int, 32>{});
+            else go(std::integral_constant<int, 8>{});
             if (const int rc = launch_status(); rc != BNN_OK) return rc;
         }
     }
@@ -179,8 +170,7 @@ BNN_EXPORT int bnn_unpack_adamw_states(const bnn_adamw_tensor* tensors, int n_te
                 continue;
             }
             hipStream_t st = static_cast<hipStream_t>(stream);
-            if (past_caches(tensors, n_tensors)) adamw_unpack_kernel<true><<<(unsigned)chunks, 256, 0, st>>>(table);
-            else adamw_unpack_kernel<false><<<(unsigned)chunks, 256, 0, st>>>(table);
+            adamw_unpack_kernel<<<grid_of(chunks), 256, 0, st>>>(table);
             if (const int rc = launch_status(); rc != BNN_OK) return rc;
         }
     }

@@ -15,7 +15,9 @@
 namespace bnn {
 
 constexpr int kAdamwTensors = 40;      // of one launch, in its arguments
-constexpr int kAdamwChunk = 4096;      // elements that a workgroup takes: 4 quads a thread
+// Elements that a workgroup takes, 4 a thread.  (16 a thread, all requested before the first is used, was slower at every size: half a million
+// elements 4.3 us against 3.6, 8-bit states 5.2 against 4.0; 1.3 million 8.5 and 7.6, 8.3 and 6.6; 29 million 134 and 131, 74.1 and 73.6.)
+constexpr int kAdamwChunk = 1024;
 
 struct AdamwTensor {
     float* w;
@@ -75,21 +77,24 @@ __device__ __forceinline__ int adamw_tensor_of(const AdamwTable& table, int chun
     return __builtin_popcountll(__builtin_amdgcn_ballot_w64(lane < table.n && table.first[lane < table.n ? lane : 0] <= chunk)) - 1;
 }
 
+// (a grid holds less than 2^32 threads along x)
+__device__ __forceinline__ int adamw_chunk_number() { return (int)(blockIdx.y * gridDim.x + blockIdx.x); }
+
 struct Quad { float v[4]; };
 // How a thread reaches its elements.  WHOLE: the chunk lies inside the tensor and its arrays are aligned; otherwise every access looks at both.
-// PAST: fp32 past the caches, for tensors that they do not hold (codes, a quarter of the size, stay).
-template <bool WHOLE, bool PAST>
+// fp32 goes past the caches, codes, a quarter of the size, stay: 29 million elements 150 -> 130 us, with 8-bit states 82.8 -> 74.2, reading those back
+// 59 -> 42; 8.4 million 45.7 -> 39.0, 23.1 -> 24.2, 14.8 -> 13.7; 4.2 million 19.0 -> 20.4, 14.1 -> 14.3, 9.2 -> 7.5; 1.3 million 7.6 -> 7.1,
+// 6.9 -> 6.4, 3.9 -> 3.1.
+template <bool WHOLE>
 struct AdamwAccess {
     typedef float v4f __attribute__((ext_vector_type(4)));
     template <class T>
     static __device__ __forceinline__ T get(const T* p) {
-        if constexpr (PAST) return __builtin_nontemporal_load(p);
-        else return *p;
+        return __builtin_nontemporal_load(p);
     }
     template <class T>
     static __device__ __forceinline__ void put(T* p, T v) {
-        if constexpr (PAST) __builtin_nontemporal_store(v, p);
-        else *p = v;
+        __builtin_nontemporal_store(v, p);
     }
     static __device__ __forceinline__ Quad load(const float* p, int64_t e, int64_t count, bool vec) {
         Quad q;
@@ -132,141 +137,112 @@ struct AdamwAccess {
 
 __device__ __forceinline__ float signed_code(uint32_t c, int j) { return (float)(int8_t)(c >> (8 * j)); }
 __device__ __forceinline__ float unsigned_code(uint32_t c, int j) { return (float)((c >> (8 * j)) & 0xFFu); }
+// the numbers that four codes of either state and their blocks' scales stand for
+__device__ __forceinline__ void adamw_numbers(uint32_t cm, uint32_t cv, uint32_t em, uint32_t ev, Quad& m, Quad& v) {
+    const float sm = mx_scale_value(em), sv = mx_scale_value(ev);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        m.v[j] = signed_code(cm, j) * sm;
+        const float r = unsigned_code(cv, j) * sv;
+        v.v[j] = r * r;
+    }
+}
 
 // The update, every operation rounded in fp32 (no contraction: the library is built with -ffp-contract=off):
 //     m' = b1 m + c1 g,   v' = b2 v + (c2 g) g,   r = sqrt(v'),   w' = w - (decay w + (size m') / (r q + eps))
-// Bound by memory: a thread requests all of its four quads before it uses the first.
-template <int BITS, bool WHOLE, bool PAST>
+// Bound by memory.
+template <int BITS, bool WHOLE>
 __device__ __forceinline__ void adamw_chunk(const AdamwTensor& t, const AdamwFactors& f, uint32_t key, int64_t chunk) {
-    using A = AdamwAccess<WHOLE, PAST>;
-    constexpr int kQuads = kAdamwChunk / 1024;
-    Quad w[kQuads], g[kQuads], m[kQuads], v[kQuads];
-    uint32_t cm[kQuads], cv[kQuads], em[kQuads], ev[kQuads];
-    const int64_t e0 = chunk + (int)threadIdx.x * 4;
-    auto inside = [&](int64_t e) { return WHOLE || (e & ~31) < t.count; };   // (whole groups of the 8 lanes of a block)
-#pragma unroll
-    for (int k = 0; k < kQuads; ++k) {
-        const int64_t e = e0 + 1024 * k;
-        if (!inside(e)) break;
-        w[k] = A::load(t.w, e, t.count, t.vec);
-        g[k] = A::load(t.g, e, t.count, t.vec);
-        if constexpr (BITS == 32) {
-            m[k] = A::load(static_cast<const float*>(t.m), e, t.count, t.vec);
-            v[k] = A::load(static_cast<const float*>(t.v), e, t.count, t.vec);
-        } else {
-            cm[k] = A::load_codes(static_cast<const unsigned char*>(t.m), e, t.count, t.vec);
-            cv[k] = A::load_codes(static_cast<const unsigned char*>(t.v), e, t.count, t.vec);
-            em[k] = t.m_scale[e >> 5];
-            ev[k] = t.v_scale[e >> 5];
-        }
+    using A = AdamwAccess<WHOLE>;
+    Quad w, g, m, v, r;
+    uint32_t em = 0, ev = 0;
+    const int64_t e = chunk + (int)threadIdx.x * 4;
+    if (!WHOLE && (e & ~31) >= t.count) return;   // (whole groups of the 8 lanes of a block)
+    w = A::load(t.w, e, t.count, t.vec);
+    g = A::load(t.g, e, t.count, t.vec);
+    if constexpr (BITS == 32) {
+        m = A::load(static_cast<const float*>(t.m), e, t.count, t.vec);
+        v = A::load(static_cast<const float*>(t.v), e, t.count, t.vec);
+    } else {
+        const uint32_t cm = A::load_codes(static_cast<const unsigned char*>(t.m), e, t.count, t.vec);
+        const uint32_t cv = A::load_codes(static_cast<const unsigned char*>(t.v), e, t.count, t.vec);
+        em = t.m_scale[e >> 5];
+        ev = t.v_scale[e >> 5];
+        adamw_numbers(cm, cv, em, ev, m, v);
     }
 #pragma unroll
-    for (int k = 0; k < kQuads; ++k) {
-        const int64_t e = e0 + 1024 * k;
-        if (!inside(e)) break;
-        Quad r;
-        if constexpr (BITS == 8) {
-            const float sm = mx_scale_value(em[k]), sv = mx_scale_value(ev[k]);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                m[k].v[j] = signed_code(cm[k], j) * sm;
-                const float old = unsigned_code(cv[k], j) * sv;
-                v[k].v[j] = old * old;
-            }
-        }
+    for (int j = 0; j < 4; ++j) {
+        const float gj = g.v[j];
+        m.v[j] = f.b1 * m.v[j] + f.c1 * gj;
+        v.v[j] = f.b2 * v.v[j] + (f.c2 * gj) * gj;
+        r.v[j] = __builtin_sqrtf(v.v[j]);
+        const float wj = w.v[j], n = wj - (f.decay * wj + (f.size * m.v[j]) / (r.v[j] * f.q + f.eps));
+        w.v[j] = t.clip ? hardtanh(n) : n;
+    }
+    A::store(t.w, e, t.count, t.vec, w);
+    if constexpr (BITS == 32) {
+        A::store(static_cast<float*>(t.m), e, t.count, t.vec, m);
+        A::store(static_cast<float*>(t.v), e, t.count, t.vec, v);
+    } else {
+        uint32_t tm = 0, tv = 0;   // (elements past the end are 0)
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const float gj = g[k].v[j];
-            m[k].v[j] = f.b1 * m[k].v[j] + f.c1 * gj;
-            v[k].v[j] = f.b2 * v[k].v[j] + (f.c2 * gj) * gj;
-            r.v[j] = __builtin_sqrtf(v[k].v[j]);
-            const float wj = w[k].v[j], n = wj - (f.decay * wj + (f.size * m[k].v[j]) / (r.v[j] * f.q + f.eps));
-            w[k].v[j] = t.clip ? hardtanh(n) : n;
+            tm = max(tm, __float_as_uint(m.v[j]) & 0x7FFFFFFFu);
+            tv = max(tv, __float_as_uint(r.v[j]) & 0x7FFFFFFFu);
         }
-        A::store(t.w, e, t.count, t.vec, w[k]);
-        if constexpr (BITS == 32) {
-            A::store(static_cast<float*>(t.m), e, t.count, t.vec, m[k]);
-            A::store(static_cast<float*>(t.v), e, t.count, t.vec, v[k]);
-        } else {
-            uint32_t tm = 0, tv = 0;   // (elements past the end are 0)
+        const uint32_t nm = mx_scale<MxInt8>(max_of_8_lanes(tm)), nv = mx_scale<MxUint8>(max_of_8_lanes(tv));
+        const float im = mx_inverse_scale(nm), iv = mx_inverse_scale(nv);
+        const uint32_t block_key = mix32(key + (uint32_t)(e >> 5));
+        uint32_t am = 0, av = 0;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                tm = max(tm, __float_as_uint(m[k].v[j]) & 0x7FFFFFFFu);
-                tv = max(tv, __float_as_uint(r.v[j]) & 0x7FFFFFFFu);
-            }
-            const uint32_t nm = mx_scale<MxInt8>(max_of_8_lanes(tm)), nv = mx_scale<MxUint8>(max_of_8_lanes(tv));
-            const float im = mx_inverse_scale(nm), iv = mx_inverse_scale(nv);
-            const uint32_t block_key = mix32(key + (uint32_t)(e >> 5));
-            uint32_t am = 0, av = 0;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const uint32_t h = mix32(block_key + (uint32_t)((e & 31) + j));
-                const int cmj = (int)(__builtin_fabsf(m[k].v[j]) * im + (float)(h & 0xFFFFu) * 0x1p-16f);
-                const int cvj = (int)(r.v[j] * iv + (float)(h >> 16) * 0x1p-16f);
-                am |= ((uint32_t)(m[k].v[j] < 0.0f ? -cmj : cmj) & 0xFFu) << (8 * j);
-                av |= ((uint32_t)cvj & 0xFFu) << (8 * j);
-            }
-            A::store_codes(static_cast<unsigned char*>(t.m), e, t.count, t.vec, nm == 255 ? 0u : am);
-            A::store_codes(static_cast<unsigned char*>(t.v), e, t.count, t.vec, nv == 255 ? 0u : av);
-            if ((threadIdx.x & 7) == 0) {
-                t.m_scale[e >> 5] = (unsigned char)nm;
-                t.v_scale[e >> 5] = (unsigned char)nv;
-            }
+        for (int j = 0; j < 4; ++j) {
+            const uint32_t h = mix32(block_key + (uint32_t)((e & 31) + j));
+            const int cmj = (int)(__builtin_fabsf(m.v[j]) * im + (float)(h & 0xFFFFu) * 0x1p-16f);
+            const int cvj = (int)(r.v[j] * iv + (float)(h >> 16) * 0x1p-16f);
+            am |= ((uint32_t)(m.v[j] < 0.0f ? -cmj : cmj) & 0xFFu) << (8 * j);
+            av |= ((uint32_t)cvj & 0xFFu) << (8 * j);
+        }
+        A::store_codes(static_cast<unsigned char*>(t.m), e, t.count, t.vec, nm == 255 ? 0u : am);
+        A::store_codes(static_cast<unsigned char*>(t.v), e, t.count, t.vec, nv == 255 ? 0u : av);
+        if ((threadIdx.x & 7) == 0) {
+            t.m_scale[e >> 5] = (unsigned char)nm;
+            t.v_scale[e >> 5] = (unsigned char)nv;
         }
     }
 }
 
 // HYPER: AdamwHost or AdamwDevice.
-template <int BITS, bool PAST, class HYPER>
+template <int BITS, class HYPER>
 __global__ __launch_bounds__(256) void adamw_kernel(const HYPER hyper, const AdamwTable table) {
-    const int i = adamw_tensor_of(table, (int)blockIdx.x);
+    const int number = adamw_chunk_number();
+    const int i = adamw_tensor_of(table, number);
     const AdamwTensor t = table.t[i];
     const AdamwFactors f = hyper.factors();
-    const int64_t chunk = (int64_t)((int)blockIdx.x - table.first[i]) * kAdamwChunk;
+    const int64_t chunk = (int64_t)(number - table.first[i]) * kAdamwChunk;
     const uint32_t key = mix32(hyper.key() + (uint32_t)(table.at + i));
-    if (t.vec && chunk + kAdamwChunk <= t.count) adamw_chunk<BITS, true, PAST>(t, f, key, chunk);
-    else adamw_chunk<BITS, false, PAST>(t, f, key, chunk);
+    if (t.vec && chunk + kAdamwChunk <= t.count) adamw_chunk<BITS, true>(t, f, key, chunk);
+    else adamw_chunk<BITS, false>(t, f, key, chunk);
 }
 
 // 8-bit states as the numbers they stand for.  In the table w is where m goes (may be absent) and g where v goes.
-template <bool WHOLE, bool PAST>
+template <bool WHOLE>
 __device__ __forceinline__ void adamw_unpack_chunk(const AdamwTensor& t, int64_t chunk) {
-    using A = AdamwAccess<WHOLE, PAST>;
-    constexpr int kQuads = kAdamwChunk / 1024;
-    uint32_t cm[kQuads], cv[kQuads], em[kQuads], ev[kQuads];
-    const int64_t e0 = chunk + (int)threadIdx.x * 4;
-#pragma unroll
-    for (int k = 0; k < kQuads; ++k) {
-        const int64_t e = e0 + 1024 * k;
-        if (!WHOLE && e >= t.count) break;
-        cm[k] = A::load_codes(static_cast<const unsigned char*>(t.m), e, t.count, t.vec);
-        cv[k] = A::load_codes(static_cast<const unsigned char*>(t.v), e, t.count, t.vec);
-        em[k] = t.m_scale[e >> 5];
-        ev[k] = t.v_scale[e >> 5];
-    }
-#pragma unroll
-    for (int k = 0; k < kQuads; ++k) {
-        const int64_t e = e0 + 1024 * k;
-        if (!WHOLE && e >= t.count) break;
-        const float sm = mx_scale_value(em[k]), sv = mx_scale_value(ev[k]);
-        Quad m, v;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            m.v[j] = signed_code(cm[k], j) * sm;
-            const float r = unsigned_code(cv[k], j) * sv;
-            v.v[j] = r * r;
-        }
-        if (t.w) A::store(t.w, e, t.count, t.vec, m);
-        if (t.g) A::store(const_cast<float*>(t.g), e, t.count, t.vec, v);
-    }
+    using A = AdamwAccess<WHOLE>;
+    const int64_t e = chunk + (int)threadIdx.x * 4;
+    if (!WHOLE && e >= t.count) return;
+    Quad m, v;
+    adamw_numbers(A::load_codes(static_cast<const unsigned char*>(t.m), e, t.count, t.vec),
+                  A::load_codes(static_cast<const unsigned char*>(t.v), e, t.count, t.vec), t.m_scale[e >> 5], t.v_scale[e >> 5], m, v);
+    if (t.w) A::store(t.w, e, t.count, t.vec, m);
+    if (t.g) A::store(const_cast<float*>(t.g), e, t.count, t.vec, v);
 }
-template <bool PAST>
 __global__ __launch_bounds__(256) void adamw_unpack_kernel(const AdamwTable table) {
-    const int i = adamw_tensor_of(table, (int)blockIdx.x);
+    const int number = adamw_chunk_number();
+    const int i = adamw_tensor_of(table, number);
     const AdamwTensor t = table.t[i];
-    const int64_t chunk = (int64_t)((int)blockIdx.x - table.first[i]) * kAdamwChunk;
-    if (t.vec && chunk + kAdamwChunk <= t.count) adamw_unpack_chunk<true, PAST>(t, chunk);
-    else adamw_unpack_chunk<false, PAST>(t, chunk);
+    const int64_t chunk = (int64_t)(number - table.first[i]) * kAdamwChunk;
+    if (t.vec && chunk + kAdamwChunk <= t.count) adamw_unpack_chunk<true>(t, chunk);
+    else adamw_unpack_chunk<false>(t, chunk);
 }
 
 }  // namespace bnn

@@ -193,20 +193,24 @@ def test_hyperparameters_on_the_device_in_a_graph(G, bnn):
                 assert same(t.get(k), e.get(k)), (bits, k)
 
 
-def test_more_than_2_to_32_elements(G, bnn):
-    n = (1 << 32) + 77
-    if torch.cuda.mem_get_info()[0] < 80 << 30:
+@pytest.mark.parametrize("n", [(1 << 32) + 77, (1 << 33) + 3 * 1024 + 77])
+def test_more_than_2_to_32_elements(G, bnn, n):
+    torch.cuda.empty_cache()
+    if torch.cuda.mem_get_info()[0] < 120 << 30:
         pytest.skip("not enough free memory")
     w, g = (torch.empty(n, device="cuda:0") for _ in range(2))
     w.uniform_(-1, 1)
     g.normal_()
     m, v = (torch.zeros(n, dtype=torch.uint8, device="cuda:0") for _ in range(2))
     ms, vs = (torch.zeros((n + 31) // 32, dtype=torch.uint8, device="cuda:0") for _ in range(2))
-    parts = [slice(0, 64), slice((1 << 31) - 32, (1 << 31) + 32), slice((1 << 32) - 64, n)]
+    parts = [slice(0, 64), slice((1 << 31) - 32, (1 << 31) + 32), slice((1 << 32) - 64, (1 << 32) + 77), slice(n - 77, n),
+             slice((n & ~4095) - 32, (n & ~4095) + 64)]
+    parts = [slice(p.start & ~31, p.stop if p.stop == n else p.stop & ~31) for p in parts]
     host = [(w[p].cpu().numpy(), g[p].cpu().numpy()) for p in parts]
     t = bnn.make_adamw_array([dict(w=w.data_ptr(), g=g.data_ptr(), m=m.data_ptr(), v=v.data_ptr(), m_scale=ms.data_ptr(), v_scale=vs.data_ptr(), count=n)])
     bnn.bnn_update_adamw(t, 1, params(bnn, 8, 1, 4), G.stream())
     first = mx.mix(mx._add(mx.mix(mx._add(mx.mix(4), 0)), 0))
+    bnn.bnn_unpack_adamw_states(t, 1, bnn.make_pointer_array([g.data_ptr()]), None, G.stream())
     for p, (hw, hg) in zip(parts, host):
         nw, nm, _, r = mx.adamw(hw, hg, np.zeros_like(hw), np.zeros_like(hw), 1)
         b = np.arange(p.start // 32, (p.stop + 31) // 32)
@@ -216,3 +220,4 @@ def test_more_than_2_to_32_elements(G, bnn):
         bs = slice(b[0], b[-1] + 1)
         assert same(w[p].cpu().numpy(), nw) and same(m[p].cpu().numpy().view(np.int8), cm.astype(np.int8)) and same(v[p].cpu().numpy(), cv.astype(np.uint8))
         assert same(ms[bs].cpu().numpy(), em) and same(vs[bs].cpu().numpy(), ev)
+        assert same(g[p].cpu().numpy(), mx.adamw_decode(cm.astype(np.int8), em).astype(np.float32))
