@@ -107,7 +107,7 @@ int run_layer(const void* Xq, const void* Wq, const float* bias, int64_t M, int6
     // 1024 x 2048 x 2048 8.6, 7.9, 9.0, 12, 17;  2048 x 2048 x 2048 13.2, 12.3, 11.0, 13.7, 18.5;  4096 x 2048 x 3400 39, 31, 26.7, 25.0, 26.5;
     // 8192 x 4096 x 3400 144, 117, 96, 91, 84.
     struct { int rows, cols, most; } const kTiles[] = {{64, 64, 256}, {128, 64, 256}, {128, 128, 512}, {256, 128, 512}, {256, 256, 0}};
-    int tile = 0;
+    int tile = N > 64 * 65535 ? 2 : 0;   // (the grid's y)
     for (; tile < 4 && tiles(kTiles[tile].rows, kTiles[tile].cols) > kTiles[tile].most; ++tile) {
         auto area = [&](int t) { return tiles(kTiles[t].rows, kTiles[t].cols) * kTiles[t].rows * kTiles[t].cols; };
         if (4 * area(tile + 1) > 5 * area(tile)) break;

@@ -387,3 +387,18 @@ def test_matrices_beyond_4_gib(G, bnn):
     back = torch.empty((R, K), device="cuda:0") if torch.cuda.mem_get_info()[0] > 40 << 30 else X
     bnn.bnn_dequantize_mx4(G.ptr(q), R, K, G.ptr(back), G.stream())
     assert np.array_equal(back[torch.from_numpy(some).to("cuda:0")].cpu().numpy(), x.astype(np.float32))
+
+
+def test_layer_of_the_most_outputs(G, bnn):
+    """As many outputs as a layer takes (2^22): exact sums at the first, the last and some columns between."""
+    M, K, N = 20, 128, 1 << 22
+    xq = random_packed(np.random.default_rng(3), M, K, whole=True)
+    wq = torch.randint(0, 256, (bnn.bnn_mx4_bytes(N, K),), dtype=torch.uint8, device="cuda:0")
+    wq[N * 64:] = 127
+    x, y = torch.from_numpy(xq).to("cuda:0"), torch.full((M, N), float("nan"), device="cuda:0")
+    bnn.bnn_layer_mx4(G.ptr(x), G.ptr(wq), 0, M, K, N, bnn.BNN_ACT_LINEAR, 32, G.ptr(y), G.stream())
+    assert bool(torch.isfinite(y).all())
+    at = torch.from_numpy(np.r_[0:70, N // 2 - 40:N // 2 + 40, 64 * 65535 - 40:N]).to("cuda:0")
+    n = at.numel()
+    some = np.concatenate([wq[:N * 64].view(N, 64)[at].cpu().numpy().reshape(-1), np.zeros(-n * 64 % 256, np.uint8), np.full(4 * n, 127, np.uint8)])
+    assert np.array_equal(y[:, at].cpu().numpy(), (mx.unpack(xq, M, K) @ mx.unpack(some, n, K).T).astype(np.float32))

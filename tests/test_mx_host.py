@@ -180,7 +180,8 @@ def test_launches_of_the_layers(host):  # noqa: F811
 result = []
 for act in (bnn.BNN_ACT_LINEAR, bnn.BNN_ACT_SIGN, bnn.BNN_ACT_LOGSOFTMAX):
     for M, K, N in ((1, 1, 1), (1, 2048, 2048), (16, 440, 1024), (17, 440, 1024), (64, 2048, 1 << 22), (65, 1 << 22, 70), (333, 1024, 3307), (4096, 2048, 2048),
-                    (16384, 4096, 4096), (1 << 30, 128, 1), (1 << 30, 128, 1000), (5, 128, 1 << 22), (1 << 22, 1 << 22, 1 << 10)):
+                    (16384, 4096, 4096), (1 << 30, 128, 1), (1 << 30, 128, 1000), (5, 128, 1 << 22), (1 << 22, 1 << 22, 1 << 10),
+                    (17, 440, 1 << 22), (64, 1024, (1 << 22) - 1), (65, 128, 1 << 22), (300, 128, 1 << 22)):
         bnn.bnn_layer_mx4(A, 1 << 55, 0, M, K, N, act, 32, 1 << 57)
         a = launches()
         need = bnn.bnn_layer_mx4_realx_workspace_bytes(M, K, N)
