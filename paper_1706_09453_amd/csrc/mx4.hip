@@ -97,20 +97,23 @@ void go_few(const void* X, const void* Wq, const float* bias, int64_t M, int64_t
 
 int run_layer(const void* Xq, const void* Wq, const float* bias, int64_t M, int64_t K, int64_t N, int act, int wb, void* Y, hipStream_t st) {
     const int yw32 = (int)row_w32(N, wb);
-    const auto tiles = [&](int rows, int cols) { return ((M + rows - 1) / rows) * ((N + cols - 1) / cols); };
     // Outputs that the caches will not hold, in rows of whole lines, are stored past them: 16384 x 4096 x 4096 190 -> 172 us, 4096 x 2048 x 2048
     // 16.4 -> 15.4.  (Rows that are no whole lines would leave as pieces of lines: 4096 x 2048 x 3400 25 -> 39 us.)
     const int nt = act != BNN_ACT_LOGSOFTMAX && N % 32 == 0 && aligned(Y, 128) && M * N >= (int64_t)8 << 20;
-    // The tile: the smallest of which no more than one (128 x 128 on: two) comes to each CU, since a workgroup's time per stage of K hardly depends on the
-    // tile while it has the CU for itself; with more of them the largest, which moves the least per product, as long as it does not take much more than the
-    // outputs there are.  us with tiles of 64 x 64, 128 x 64, 128 x 128, 256 x 128, 256 x 256:  333 x 1024 x 3400 5.1, 5.2, 5.8, 8.0, 11.4;
-    // 1024 x 2048 x 2048 8.6, 7.9, 9.0, 12, 17;  2048 x 2048 x 2048 13.2, 12.3, 11.0, 13.7, 18.5;  4096 x 2048 x 3400 39, 31, 26.7, 25.0, 26.5;
-    // 8192 x 4096 x 3400 144, 117, 96, 91, 84.
-    struct { int rows, cols, most; } const kTiles[] = {{64, 64, 256}, {128, 64, 256}, {128, 128, 512}, {256, 128, 512}, {256, 256, 0}};
-    int tile = N > 64 * 65535 ? 2 : 0;   // (the grid's y)
-    for (; tile < 4 && tiles(kTiles[tile].rows, kTiles[tile].cols) > kTiles[tile].most; ++tile) {
-        auto area = [&](int t) { return tiles(kTiles[t].rows, kTiles[t].cols) * kTiles[t].rows * kTiles[t].cols; };
-        if (4 * area(tile + 1) > 5 * area(tile)) break;
+    // The tile: the one with the least time by a straight line per round of 256 tiles (us: `round` and `chunk` of each), fitted to 162 products
+    // measured with each of the five (256 to 16384 frames, 512 to 4096 inputs, 1000 to 4096 outputs, fp32 and Sign outputs: the tile chosen takes 1.7 %
+    // more than the best one on average, 12 % at most).  Below 768 inputs the first three, as the outputs of a large tile leave when its products are
+    // done, and few products hide them: 8192 x 512 x 4096 30.2 us with tiles of 128 x 128, 32.8 with 256 x 256.  us with tiles of 64 x 64, 128 x 64,
+    // 128 x 128, 256 x 128, 256 x 256:  512 x 2048 x 2048 6.2, 7.1, 8.6, 11.2, 15.7;  2048 x 2048 x 2048 14.0, 12.8, 12.0, 13.7, 17.9;  2048 x 4096 x 3400 38,
+    // 34, 26.9, 25.3, 29.8;  4096 x 2048 x 3400 39, 32, 29.3, 30.1, 26.5;  8192 x 4096 x 3400 140, 111, 87, 91, 73.
+    struct { int rows, cols; double round, chunk; } const kTiles[] = {{64, 64, 0.14, 0.14}, {128, 64, 0.34, 0.22}, {128, 128, 0.98, 0.31}, {256, 128, 2.25, 0.48}, {256, 256, 3.9, 0.64}};
+    int tile = 0;
+    double least = 0.0;
+    for (int t = 0; t < (K < 768 ? 3 : 5); ++t) {
+        const int64_t gx = (M + kTiles[t].rows - 1) / kTiles[t].rows, gy = (N + kTiles[t].cols - 1) / kTiles[t].cols;
+        if (gx > 1 << 23 || gy > 65535) continue;   // (2^31 threads along x; 2^30 frames of 128, 2^22 outputs of 128 are inside)
+        const double time = (double)((gx * gy + 255) / 256) * (kTiles[t].round + kTiles[t].chunk * (double)mx4_chunks(K));
+        if (least == 0.0 || time < least) tile = t, least = time;
     }
     bool ok = true;
     auto go = [&](auto a) {
@@ -118,7 +121,7 @@ int run_layer(const void* Xq, const void* Wq, const float* bias, int64_t M, int6
         if (tile == 0) ok = launch_gemm<1, 1, 2, 2, 4, A>(Xq, Wq, bias, (int)M, (int)K, (int)N, Y, yw32, nt, st);
         else if (tile == 1) ok = launch_gemm<2, 1, 2, 2, 4, A>(Xq, Wq, bias, (int)M, (int)K, (int)N, Y, yw32, nt, st);
         else if (tile == 2) ok = launch_gemm<2, 2, 2, 2, 3, A>(Xq, Wq, bias, (int)M, (int)K, (int)N, Y, yw32, nt, st);
-        else if (tile == 3) ok = launch_gemm<4, 2, 2, 2, 3, A>(Xq, Wq, bias, (int)M, (int)K, (int)N, Y, yw32, nt, st);
+        else if (tile == 3) ok = launch_gemm<2, 2, 4, 2, 4, A>(Xq, Wq, bias, (int)M, (int)K, (int)N, Y, yw32, nt, st);
         else ok = launch_gemm<4, 2, 2, 4, 4, A>(Xq, Wq, bias, (int)M, (int)K, (int)N, Y, yw32, nt, st);
     };
     if (few_frames(M, K)) go_few<false>(Xq, Wq, bias, M, K, N, act, Y, yw32, false, st);

@@ -197,3 +197,18 @@ for R, C in ((1, 1), (1 << 30, 1), (1, 1 << 30), (1 << 20, 1 << 20), (1 << 30, 1
         if act >= 0:
             soft = act == 4
             assert len(a) == 1 + soft and len(b) in (1 + soft, 2 + soft)
+
+
+def test_sizes_reach_every_tile(host):  # noqa: F811
+    """The sizes that the layers are tested at on the device take each of the product's tiles."""
+    from test_gpu_mx4 import LAYERS
+    got = host("""
+result = []
+for M, K, N in %r:
+    bnn.bnn_layer_mx4(A, 1 << 55, 0, M, K, N, bnn.BNN_ACT_LINEAR, 32, 1 << 57)
+    result.append(launches()[0]["kernel"])
+""" % (LAYERS,))
+    tiles = {k.split("mx4_gemm_kernelI")[1][:20] for k in got if "mx4_gemm_kernel" in k}
+    assert tiles == {"Li1ELi1ELi2ELi2ELi4E", "Li2ELi1ELi2ELi2ELi4E", "Li2ELi2ELi2ELi2ELi3E", "Li2ELi2ELi4ELi2ELi4E", "Li4ELi2ELi2ELi4ELi4E"}
+    few = {k.split("mx4_few_kernelI")[1][:4] for k in got if "mx4_few_kernel" in k}
+    assert few == {"Li1E", "Li2E", "Li4E"}
