@@ -42,15 +42,15 @@ int run_quantize(const float* X, int64_t R, int64_t C, bool stochastic, const Mx
     return launch_status();
 }
 
-template <int FM, int FN, int WAVES_M, int WAVES_N, int STAGES, int ACT>
+template <int FM, int FN, int WAVES_M, int WAVES_N, int STAGES, int ACT, bool RUN = false>
 bool launch_gemm(const void* Xq, const void* Wq, const float* bias, int M, int K, int N, void* Y, int yw32, int nt, hipStream_t st) {
-    using T = Mx4Tile<FM, FN, WAVES_M, WAVES_N, STAGES>;
-    const auto kernel = mx4_gemm_kernel<FM, FN, WAVES_M, WAVES_N, STAGES, ACT>;
+    using T = Mx4Tile<FM, FN, WAVES_M, WAVES_N, STAGES, RUN>;
+    const auto kernel = mx4_gemm_kernel<FM, FN, WAVES_M, WAVES_N, STAGES, ACT, RUN>;
     if constexpr (T::kLds > 65536) {
         static std::atomic<uint64_t> allowed{0};
         if (!allow_lds(kernel, T::kLds, allowed)) return false;
     }
-    const dim3 grid((unsigned)((M + T::kRows - 1) / T::kRows), (unsigned)((N + T::kCols - 1) / T::kCols));
+    const dim3 tiles((unsigned)((M + T::kRows - 1) / T::kRows), (unsigned)((N + T::kCols - 1) / T::kCols)), grid = RUN ? dim3(kMx4Groups) : tiles;
     kernel<<<grid, T::kThreads, T::kLds, st>>>(Xq, Wq, bias, M, K, N, (int)mx4_chunks(K), Y, yw32, nt);
     return true;
 }
@@ -115,6 +115,10 @@ int run_layer(const void* Xq, const void* Wq, const float* bias, int64_t M, int6
         const double time = (double)((gx * gy + 255) / 256) * (kTiles[t].round + kTiles[t].chunk * (double)mx4_chunks(K));
         if (least == 0.0 || time < least) tile = t, least = time;
     }
+// From the third round of the largest tile on a workgroup per CU stays for all of its tiles, so that neither the first stages of a tile nor the outputs
+    // of the one before stand alone: 16384 x 1024 x 4096 71 -> 67 us (to Sign 49 -> 44), 65536 x 2048 x 2048 185 -> 175, 16384 x 4096 x 4096 156 -> 153, where power
+    // is what bounds it.  (In two rounds the CUs with one tile wait for those with two either way: 8192 x 4096 x 3400 73 -> 75.)
+    const bool run = tile == 4 && ((M + 255) / 256) * ((N + 255) / 256) > 2 * kMx4Groups && mx4_chunks(K) >= 8;
     bool ok = true;
     auto go = [&](auto a) {
         constexpr int A = decltype(a)::value;
@@ -122,6 +126,7 @@ int run_layer(const void* Xq, const void* Wq, const float* bias, int64_t M, int6
         else if (tile == 1) ok = launch_gemm<2, 1, 2, 2, 4, A>(Xq, Wq, bias, (int)M, (int)K, (int)N, Y, yw32, nt, st);
         else if (tile == 2) ok = launch_gemm<2, 2, 2, 2, 3, A>(Xq, Wq, bias, (int)M, (int)K, (int)N, Y, yw32, nt, st);
         else if (tile == 3) ok = launch_gemm<2, 2, 4, 2, 4, A>(Xq, Wq, bias, (int)M, (int)K, (int)N, Y, yw32, nt, st);
+        else if (run) ok = launch_gemm<4, 2, 2, 4, 4, A, true>(Xq, Wq, bias, (int)M, (int)K, (int)N, Y, yw32, nt, st);
         else ok = launch_gemm<4, 2, 2, 4, 4, A>(Xq, Wq, bias, (int)M, (int)K, (int)N, Y, yw32, nt, st);
     };
     if (few_frames(M, K)) go_few<false>(Xq, Wq, bias, M, K, N, act, Y, yw32, false, st);

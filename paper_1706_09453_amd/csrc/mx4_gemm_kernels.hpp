@@ -22,12 +22,15 @@ __device__ __forceinline__ float mx4_act(float h) {
 // Both operands of a workgroup's tile go to LDS by loads that write it directly, in stages of a chunk (128 elements: 64 bytes of codes and a
 // word of scale bytes per row), STAGES of them in rotation.  In LDS a row's four 16-byte pieces lie at piece ^ (row / 4 % 4), so that the 16
 // lanes that are served together read 16 different places of the 64 banks.
-template <int FM, int FN, int WAVES_M, int WAVES_N, int STAGES>
+// RUN: a workgroup per CU takes every kMx4Groups'th tile, the stages of one behind those of the other without a gap: the next tile's first stages
+// are on their way before the last products of a tile, and its outputs leave beside the next one's first products.
+constexpr int kMx4Groups = 256;
+template <int FM, int FN, int WAVES_M, int WAVES_N, int STAGES, bool RUN>
 struct Mx4Tile {
     static constexpr int kWaves = WAVES_M * WAVES_N, kThreads = 64 * kWaves;
     static constexpr int kRows = 32 * FM * WAVES_M, kCols = 32 * FN * WAVES_N;   // frames and outputs of a workgroup
     static constexpr int kCodes = (kRows + kCols) * 64, kStage = kCodes + (kRows + kCols) * 4;
-    static constexpr unsigned kLds = (unsigned)STAGES * kStage + kCols * 4;   // stages; bias
+    static constexpr unsigned kLds = (unsigned)STAGES * kStage + (RUN ? 2 : 1) * kCols * 4;   // stages; bias
     static constexpr int kAL = kRows / 16 / kWaves, kBL = kCols / 16 / kWaves;   // loads of 16 rows per wave and stage
     static constexpr int kScaleLoads = (kRows + kCols) / 64;                     // loads of 64 scale words per stage, and
     static constexpr int kSL = (kScaleLoads + kWaves - 1) / kWaves;              // per wave (some twice, so that all waves have as many)
@@ -35,36 +38,48 @@ struct Mx4Tile {
     static_assert(kRows % (16 * kWaves) == 0 && kCols % (16 * kWaves) == 0 && kRows % 64 == 0 && kCols % 64 == 0 && kCols / 64 <= kWaves);
 };
 
-template <int FM, int FN, int WAVES_M, int WAVES_N, int STAGES, int ACT>
-__global__ __launch_bounds__(64 * WAVES_M * WAVES_N, FM * FN > 8 ? 1 : 2) void mx4_gemm_kernel(const void* __restrict__ Xq, const void* __restrict__ Wq,
+template <int FM, int FN, int WAVES_M, int WAVES_N, int STAGES, int ACT, bool RUN>
+__global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void mx4_gemm_kernel(const void* __restrict__ Xq, const void* __restrict__ Wq,
                                                                          const float* __restrict__ bias, int M, int K, int N, int chunks,
                                                                          void* __restrict__ Y, int yw32, int nt) {
-    using T = Mx4Tile<FM, FN, WAVES_M, WAVES_N, STAGES>;
+    using T = Mx4Tile<FM, FN, WAVES_M, WAVES_N, STAGES, RUN>;
     extern __shared__ __attribute__((aligned(16))) unsigned char mx4_mem[];
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = lane_id(), r = lane & 31, g = lane >> 5;
     const int wm = wave / WAVES_N, wn = wave % WAVES_N;
-    int tile_m, tile_n;
-    xcd_tile(tile_m, tile_n);
-    const int m0 = tile_m * T::kRows, n0 = tile_n * T::kCols;
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)mx4_mem;
+    const int tiles_m = (M + T::kRows - 1) / T::kRows, tiles_n = (N + T::kCols - 1) / T::kCols;
+    int tile_m, tile_n;
+    if constexpr (RUN) xcd_tile((int)blockIdx.x, tiles_m, tiles_n, tile_m, tile_n);
+    else xcd_tile(tile_m, tile_n);
+    int m0 = tile_m * T::kRows, n0 = tile_n * T::kCols;
 
     // ---- the wave's share of a stage's loads: rows in pieces of 16 bytes, four lanes a row; scale words, one lane a row.  Rows past the
     // last one repeat it.
-    const int row_bytes = chunks * 64;
-    const i32x4m xr = raw_buffer(static_cast<const unsigned char*>(Xq) + (size_t)m0 * row_bytes, 0x7FFFFFFFu);
-    const i32x4m wr = raw_buffer(static_cast<const unsigned char*>(Wq) + (size_t)n0 * row_bytes, 0x7FFFFFFFu);
-    const uint32_t *xs = mx4_scales(Xq, M, K) + m0, *ws = mx4_scales(Wq, N, K) + n0;
-    const int piece = ((lane & 3) ^ ((lane >> 4) & 3)) * 16;
+    const int row_bytes = chunks * 64, piece = ((lane & 3) ^ ((lane >> 4) & 3)) * 16;
+    i32x4m xr, wr;
+    const uint32_t *xs, *ws;
     int xo[T::kAL], wo[T::kBL], so[T::kSL];
+    auto aim = [&](int m0, int n0) {   // at a tile
+        xr = raw_buffer(static_cast<const unsigned char*>(Xq) + (size_t)m0 * row_bytes, 0x7FFFFFFFu);
+        wr = raw_buffer(static_cast<const unsigned char*>(Wq) + (size_t)n0 * row_bytes, 0x7FFFFFFFu);
+        xs = mx4_scales(Xq, M, K) + m0;
+        ws = mx4_scales(Wq, N, K) + n0;
 #pragma unroll
-    for (int i = 0; i < T::kAL; ++i) xo[i] = min((wave * T::kAL + i) * 16 + (lane >> 2), M - 1 - m0) * row_bytes + piece;
+        for (int i = 0; i < T::kAL; ++i) xo[i] = min((wave * T::kAL + i) * 16 + (lane >> 2), M - 1 - m0) * row_bytes + piece;
 #pragma unroll
-    for (int i = 0; i < T::kBL; ++i) wo[i] = min((wave * T::kBL + i) * 16 + (lane >> 2), N - 1 - n0) * row_bytes + piece;
+        for (int i = 0; i < T::kBL; ++i) wo[i] = min((wave * T::kBL + i) * 16 + (lane >> 2), N - 1 - n0) * row_bytes + piece;
 #pragma unroll
-    for (int i = 0; i < T::kSL; ++i) {
-        const int row = (wave * T::kSL + i) % T::kScaleLoads * 64 + lane;   // frames rows first: a load has rows of one kind only
-        so[i] = (row < T::kRows ? min(row, M - 1 - m0) : min(row - T::kRows, N - 1 - n0)) * 4;
-    }
+        for (int i = 0; i < T::kSL; ++i) {
+            const int row = (wave * T::kSL + i) % T::kScaleLoads * 64 + lane;   // frames rows first: a load has rows of one kind only
+            so[i] = (row < T::kRows ? min(row, M - 1 - m0) : min(row - T::kRows, N - 1 - n0)) * 4;
+        }
+    };
+    // the bias of the tile's columns, in front of its first stage
+    auto request_bias = [&](int n0, int place) {
+        if (bias && wave < T::kCols / 64)
+            load_lds4(raw_buffer(bias + n0, 0x7FFFFFFFu), min(wave * 64 + lane, N - 1 - n0) * 4, 0, lds0 + (uint32_t)(STAGES * T::kStage + place * T::kCols * 4 + wave * 256));
+    };
+    aim(m0, n0);
     auto request_one = [&](int l, int c, int slot) {   // load l of the wave's kLoads of stage c
         const uint32_t base = lds0 + (uint32_t)(slot * T::kStage);
         if (l < T::kAL) {
@@ -82,9 +97,7 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, FM * FN > 8 ? 1 : 2) void m
 #pragma unroll
         for (int l = 0; l < T::kLoads; ++l) request_one(l, c, slot);
     };
-    // the bias of the tile's columns, in front of the first stage
-    if (bias && wave < T::kCols / 64)
-        load_lds4(raw_buffer(bias + n0, 0x7FFFFFFFu), min(wave * 64 + lane, N - 1 - n0) * 4, 0, lds0 + (uint32_t)(STAGES * T::kStage + wave * 256));
+    request_bias(n0, 0);
 #pragma unroll
     for (int c = 0; c < STAGES; ++c)
         if (c < chunks) request(c, c);
@@ -94,17 +107,23 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, FM * FN > 8 ? 1 : 2) void m
         asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((STAGES - 2) * T::kLoads) : "memory");
         __builtin_amdgcn_sched_barrier(0);
     };
+    // (RUN, a tile's first stages: the outputs of the tile before, at least 63 stores, are behind what is waited for)
+    static_assert(!RUN || FM * FN * 16 >= 63);
+    auto first_turn = [&]() {
+        asm volatile("s_waitcnt vmcnt(63) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+    };
     auto last_turn = [&]() {
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
         __builtin_amdgcn_sched_barrier(0);
     };
     const int steady = chunks > STAGES ? chunks - STAGES : 0;
     auto next_slot = [](int s) { return s == STAGES - 1 ? 0 : s + 1; };
-    const int m_base = m0 + wm * (32 * FM), n_base = n0 + wn * (32 * FN);
+    int m_base = m0 + wm * (32 * FM), n_base = n0 + wn * (32 * FN);
     if (STAGES <= chunks) asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"((STAGES - 1) * T::kLoads) : "memory");
     else asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
     __builtin_amdgcn_sched_barrier(0);
-    if (m_base >= M || (ACT == ACT_SIGN ? n_base >= 32 * yw32 : n_base >= N)) {   // wave-uniform: nothing to write, but its share of the stages to bring
+    if (!RUN && (m_base >= M || (ACT == ACT_SIGN ? n_base >= 32 * yw32 : n_base >= N))) {   // wave-uniform: nothing to write, but its share of the stages to bring
         int c = 0;
         for (int slot = 0; c < steady; ++c, slot = next_slot(slot)) {
             turn();
@@ -114,12 +133,6 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, FM * FN > 8 ? 1 : 2) void m
         return;
     }
     v16f acc[FM][FN];
-#pragma unroll
-    for (int i = 0; i < FM; ++i)
-#pragma unroll
-        for (int j = 0; j < FN; ++j)
-#pragma unroll
-            for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.0f;
     const int arow = wm * (32 * FM) + r, brow = T::kRows + wn * (32 * FN) + r;
     const int p0 = (g ^ ((r >> 2) & 3)) * 16, p1 = ((2 + g) ^ ((r >> 2) & 3)) * 16;
     // the lane's blocks of one of a stage's two steps, fragment f of FN + FM, and its scale words
@@ -142,10 +155,10 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, FM * FN > 8 ? 1 : 2) void m
     for (int f = 0; f < F; ++f) fetch_one(f, a0, b0, 0, p0);
 #pragma unroll
     for (int f = 0; f < F; ++f) fetch_scale(f, na, nb, 0);
-    int c = 0, slot = 0;
+    int c = 0, slot = 0, wanted = STAGES;   // stage of the tile, its place, stage that is requested next
     // A wave issues in order, and a product that finds the matrix core busy (32 clocks each) holds up what follows it: what else a stage
     // asks for is spread over the products, a slot behind each, pinned by scheduling barriers.
-    auto stage = [&](auto more) {   // more: stage c + STAGES is requested
+    auto stage = [&](auto more, auto first) {   // more: a stage is requested; first: of a tile, behind another
         const int nslot = next_slot(slot);
 #pragma unroll
         for (int j = 0; j < FN; ++j) sb[j] = nb[j] >> (8 * g);   // bytes 0 and 2: the lane's blocks of the two steps
@@ -160,7 +173,8 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, FM * FN > 8 ? 1 : 2) void m
             for (int f = q * kEach; f < (q + 1) * kEach && f < F; ++f) fetch_one(f, a1, b1, slot, p1);
             __builtin_amdgcn_sched_barrier(0);
         }
-        if constexpr (decltype(more)::value) turn();
+        if constexpr (decltype(first)::value) first_turn();
+        else if constexpr (decltype(more)::value) turn();
         else last_turn();
         const int from = decltype(more)::value || c + 1 < chunks ? nslot : slot;   // (behind the last stage: read again, unused)
 #pragma unroll
@@ -175,86 +189,133 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, FM * FN > 8 ? 1 : 2) void m
             if constexpr (decltype(more)::value) {
                 if (q >= kFrom) {
 #pragma unroll
-                    for (int l = (q - kFrom) * T::kLoads / kRest; l < (q - kFrom + 1) * T::kLoads / kRest; ++l) request_one(l, c + STAGES, slot);
+                    for (int l = (q - kFrom) * T::kLoads / kRest; l < (q - kFrom + 1) * T::kLoads / kRest; ++l) request_one(l, wanted, slot);
                 }
             }
             __builtin_amdgcn_sched_barrier(0);
         }
         slot = nslot;
         ++c;
+        ++wanted;
     };
-    while (c < steady) stage(std::true_type{});
-    do stage(std::false_type{});
-    while (c < chunks);
     // register v of lane (r, g): row 8 (v / 4) + 4 g + v % 4, column r.  Stores go through a buffer that begins at the fragment's first row and
     // ends with the matrix, so that rows past M fall away; columns past N get an offset past its end.
-    const float* bias_s = reinterpret_cast<const float*>(mx4_mem + STAGES * T::kStage) + wn * (32 * FN) + r;
-    if constexpr (ACT == ACT_SIGN) {
-        // A lane gathers the bits of its column over the rows of two fragments, and the 32 x 32 bits of a half wave are transposed: a word per lane.
-        static_assert(FN <= 2, "TransposeBits takes what a lane stores together");
-        const TransposeBits transposed(lane);
+    auto finish = [&](int place) {
+        const float* bias_s = reinterpret_cast<const float*>(mx4_mem + STAGES * T::kStage + place * T::kCols * 4) + wn * (32 * FN) + r;
+        if constexpr (ACT == ACT_SIGN) {
+            // A lane gathers the bits of its column over the rows of two fragments, and the 32 x 32 bits of a half wave are transposed: a word per lane.
+            static_assert(FN <= 2, "TransposeBits takes what a lane stores together");
+            const TransposeBits transposed(lane);
 #pragma unroll
-        for (int p = 0; p < (FM + 1) / 2; ++p) {
-            uint32_t w[FN];
-#pragma unroll
-            for (int j = 0; j < FN; ++j) {
-                const float b = bias ? bias_s[32 * j] : 0.0f;
-                w[j] = 0u;
-#pragma unroll
-                for (int i = 0; i < (FM > 1 ? 32 : 16); ++i)   // bit i: row 8 (v / 4) + 4 g + v % 4 of fragment 2 p + i / 16, v = i % 16
-                    w[j] |= sign_bit(acc[2 * p + (i >> 4)][j][i & 15] + b) ? 1u << i : 0u;
-                w[j] = n_base + 32 * j + r < N ? w[j] : 0u;
-            }
-            transposed.run(w);
-            const int v = r & 15, m = m_base + (2 * p + (r >> 4)) * 32 + 8 * (v >> 2) + 4 * g + (v & 3);
-            if (m < M && (FM > 1 || r < 16)) {
-#pragma unroll
-                for (int j = 0; j < FN; ++j)
-                    if ((n_base >> 5) + j < yw32) static_cast<uint32_t*>(Y)[(size_t)m * yw32 + (n_base >> 5) + j] = w[j];
-            }
-        }
-        return;
-    }
-    // Two fragments side by side exchange half waves, so that a store writes 64 columns of one row (32 of two rows in pieces of a line each
-    // where rows are no whole lines: 8192 x 2048 x 3400 65 us, 54 so).
-    float b[FN];
-#pragma unroll
-    for (int j = 0; j < FN; ++j) b[j] = bias ? bias_s[32 * j] : 0.0f;
-    constexpr bool kPairs = FN % 2 == 0;
-#pragma unroll
-    for (int i = 0; i < FM; ++i) {
-        const int m = m_base + 32 * i;
-        const int stride = N * 4, rows = __builtin_amdgcn_readfirstlane(min(max(M - m, 0), 32));   // (32 rows of 2^22 columns: 2^29 bytes)
-        const uint64_t first = reinterpret_cast<uint64_t>(Y) + (size_t)min(m, M) * N * 4;
-        const uint64_t low = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)first), high = (uint32_t)__builtin_amdgcn_readfirstlane((int)(first >> 32));
-        const auto out = __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>(low | high << 32), 0, rows * stride, 0x00020000);
-        auto store = [&](auto policy) {
-            constexpr int P = decltype(policy)::value;
-            if constexpr (kPairs) {
-#pragma unroll
-                for (int j = 0; j < FN; j += 2) {
-                    const int n = n_base + 32 * j + lane, at = n < N ? n * 4 : 0x7FFFFFFF;
-#pragma unroll
-                    for (int v = 0; v < 16; ++v) {
-                        const auto pair = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx4_act<ACT>(acc[i][j][v] + b[j])),
-                                                                           __float_as_uint(mx4_act<ACT>(acc[i][j + 1][v] + b[j + 1])), false, false);
-                        const int row = 8 * (v >> 2) + (v & 3);
-                        __builtin_amdgcn_raw_buffer_store_b32(pair[0], out, at, row * stride, P);
-                        __builtin_amdgcn_raw_buffer_store_b32(pair[1], out, at, (row + 4) * stride, P);
-                    }
-                }
-            } else {
+            for (int p = 0; p < (FM + 1) / 2; ++p) {
+                uint32_t w[FN];
 #pragma unroll
                 for (int j = 0; j < FN; ++j) {
-                    const int n = n_base + 32 * j + r, at = n < N ? 4 * g * stride + n * 4 : 0x7FFFFFFF;
+                    const float b = bias ? bias_s[32 * j] : 0.0f;
+                    w[j] = 0u;
 #pragma unroll
-                    for (int v = 0; v < 16; ++v)
-                        __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(mx4_act<ACT>(acc[i][j][v] + b[j])), out, at, (8 * (v >> 2) + (v & 3)) * stride, P);
+                    for (int i = 0; i < (FM > 1 ? 32 : 16); ++i)   // bit i: row 8 (v / 4) + 4 g + v % 4 of fragment 2 p + i / 16, v = i % 16
+                        w[j] |= sign_bit(acc[2 * p + (i >> 4)][j][i & 15] + b) ? 1u << i : 0u;
+                    w[j] = n_base + 32 * j + r < N ? w[j] : 0u;
+                }
+                transposed.run(w);
+                const int v = r & 15, m = m_base + (2 * p + (r >> 4)) * 32 + 8 * (v >> 2) + 4 * g + (v & 3);
+                if (m < M && (FM > 1 || r < 16)) {
+#pragma unroll
+                    for (int j = 0; j < FN; ++j)
+                        if ((n_base >> 5) + j < yw32) static_cast<uint32_t*>(Y)[(size_t)m * yw32 + (n_base >> 5) + j] = w[j];
                 }
             }
-        };
-        if (nt) store(std::integral_constant<int, 2>{});   // past the caches
-        else store(std::integral_constant<int, 0>{});
+            return;
+        }
+        // Two fragments side by side exchange half waves, so that a store writes 64 columns of one row (32 of two rows in pieces of a line each
+        // where rows are no whole lines: 8192 x 2048 x 3400 65 us, 54 so).
+        float b[FN];
+#pragma unroll
+        for (int j = 0; j < FN; ++j) b[j] = bias ? bias_s[32 * j] : 0.0f;
+        constexpr bool kPairs = FN % 2 == 0;
+#pragma unroll
+        for (int i = 0; i < FM; ++i) {
+            const int m = m_base + 32 * i;
+            int stride = N * 4;
+            if constexpr (RUN) asm volatile("" : "+s"(stride));   // (its multiples are made here, not held over the tiles)
+            const int rows = __builtin_amdgcn_readfirstlane(min(max(M - m, 0), 32));   // (32 rows of 2^22 columns: 2^29 bytes)
+            const uint64_t first = reinterpret_cast<uint64_t>(Y) + (size_t)min(m, M) * N * 4;
+            const uint64_t low = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)first), high = (uint32_t)__builtin_amdgcn_readfirstlane((int)(first >> 32));
+            const auto out = __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>(low | high << 32), 0, rows * stride, 0x00020000);
+            auto store = [&](auto policy) {
+                constexpr int P = decltype(policy)::value;
+                if constexpr (kPairs) {
+#pragma unroll
+                    for (int j = 0; j < FN; j += 2) {
+                        const int n = n_base + 32 * j + lane, at = n < N ? n * 4 : 0x7FFFFFFF;
+#pragma unroll
+                        for (int v = 0; v < 16; ++v) {
+                            const auto pair = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx4_act<ACT>(acc[i][j][v] + b[j])),
+                                                                               __float_as_uint(mx4_act<ACT>(acc[i][j + 1][v] + b[j + 1])), false, false);
+                            const int row = 8 * (v >> 2) + (v & 3);
+                            __builtin_amdgcn_raw_buffer_store_b32(pair[0], out, at, row * stride, P);
+                            __builtin_amdgcn_raw_buffer_store_b32(pair[1], out, at, (row + 4) * stride, P);
+                            // (stores that come as fast as they can hold up the next tile's loads: 16384 x 1024 x 4096 73 us, 67.5 so)
+                            if constexpr (RUN) asm volatile("s_nop 7");
+                        }
+                    }
+                } else {
+#pragma unroll
+                    for (int j = 0; j < FN; ++j) {
+                        const int n = n_base + 32 * j + r, at = n < N ? 4 * g * stride + n * 4 : 0x7FFFFFFF;
+#pragma unroll
+                        for (int v = 0; v < 16; ++v)
+                            __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(mx4_act<ACT>(acc[i][j][v] + b[j])), out, at, (8 * (v >> 2) + (v & 3)) * stride, P);
+                    }
+                }
+            };
+            if (nt) store(std::integral_constant<int, 2>{});   // past the caches
+            else store(std::integral_constant<int, 0>{});
+        }
+    };
+    auto clear = [&]() {
+#pragma unroll
+        for (int i = 0; i < FM; ++i)
+#pragma unroll
+            for (int j = 0; j < FN; ++j)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.0f;
+    };
+    using Yes = std::true_type;
+    using No = std::false_type;
+    if constexpr (!RUN) {
+        clear();
+        while (c < steady) stage(Yes{}, No{});
+        do stage(No{}, No{});
+        while (c < chunks);
+        finish(0);
+    } else {   // (at least 2 STAGES chunks)
+        const int total = tiles_m * tiles_n;
+        int first = 0, place = 0;
+        for (int id = (int)blockIdx.x;;) {
+            const int next = id + kMx4Groups < total ? id + kMx4Groups : id;   // (behind the last tile its first stages come once more, unused)
+            clear();
+            while (c < first) stage(Yes{}, std::integral_constant<bool, ACT != ACT_SIGN>{});   // (of Sign outputs few are behind)
+            do {
+                if (c == steady) {
+                    xcd_tile(next, tiles_m, tiles_n, tile_m, tile_n);
+                    aim(tile_m * T::kRows, tile_n * T::kCols);
+                    request_bias(tile_n * T::kCols, place ^ 1);
+                    wanted = 0;
+                }
+                stage(Yes{}, No{});
+            } while (c < chunks);
+            finish(place);
+            if (next == id) break;
+            id = next;
+            m_base = tile_m * T::kRows + wm * (32 * FM);
+            n_base = tile_n * T::kCols + wn * (32 * FN);
+            place ^= 1;
+            first = STAGES - 1;
+            c = 0;
+        }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // (nothing may arrive in LDS behind the end)
     }
 }
 

@@ -208,7 +208,9 @@ for M, K, N in %r:
     bnn.bnn_layer_mx4(A, 1 << 55, 0, M, K, N, bnn.BNN_ACT_LINEAR, 32, 1 << 57)
     result.append(launches()[0]["kernel"])
 """ % (LAYERS,))
-    tiles = {k.split("mx4_gemm_kernelI")[1][:20] for k in got if "mx4_gemm_kernel" in k}
+    gemm = [k.split("mx4_gemm_kernelI")[1] for k in got if "mx4_gemm_kernel" in k]   # ... activation, a workgroup per CU for all its tiles
+    assert {k[20:].split("E")[1] for k in gemm} == {"Lb0", "Lb1"}
+    tiles = {k[:20] for k in gemm}
     assert tiles == {"Li1ELi1ELi2ELi2ELi4E", "Li2ELi1ELi2ELi2ELi4E", "Li2ELi2ELi2ELi2ELi3E", "Li2ELi2ELi4ELi2ELi4E", "Li4ELi2ELi2ELi4ELi4E"}
     few = {k.split("mx4_few_kernelI")[1][:4] for k in got if "mx4_few_kernel" in k}
     assert few == {"Li1E", "Li2E", "Li4E"}
