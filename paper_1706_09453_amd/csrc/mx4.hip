@@ -100,22 +100,22 @@ int run_layer(const void* Xq, const void* Wq, const float* bias, int64_t M, int6
     // Outputs that the caches will not hold, in rows of whole lines, are stored past them: 16384 x 4096 x 4096 190 -> 172 us, 4096 x 2048 x 2048
     // 16.4 -> 15.4.  (Rows that are no whole lines would leave as pieces of lines: 4096 x 2048 x 3400 25 -> 39 us.)
     const int nt = act != BNN_ACT_LOGSOFTMAX && N % 32 == 0 && aligned(Y, 128) && M * N >= (int64_t)8 << 20;
-    // The tile: the one with the least time by a straight line per round of 256 tiles (us: `round` and `chunk` of each), fitted to 162 products
-    // measured with each of the five (256 to 16384 frames, 512 to 4096 inputs, 1000 to 4096 outputs, fp32 and Sign outputs: the tile chosen takes 1.7 %
-    // more than the best one on average, 12 % at most).  Below 768 inputs the first three, as the outputs of a large tile leave when its products are
-    // done, and few products hide them: 8192 x 512 x 4096 30.2 us with tiles of 128 x 128, 32.8 with 256 x 256.  us with tiles of 64 x 64, 128 x 64,
-    // 128 x 128, 256 x 128, 256 x 256:  512 x 2048 x 2048 6.2, 7.1, 8.6, 11.2, 15.7;  2048 x 2048 x 2048 14.0, 12.8, 12.0, 13.7, 17.9;  2048 x 4096 x 3400 38,
-    // 34, 26.9, 25.3, 29.8;  4096 x 2048 x 3400 39, 32, 29.3, 30.1, 26.5;  8192 x 4096 x 3400 140, 111, 87, 91, 73.
-    struct { int rows, cols; double round, chunk; } const kTiles[] = {{64, 64, 0.14, 0.14}, {128, 64, 0.34, 0.22}, {128, 128, 0.98, 0.31}, {256, 128, 2.25, 0.48}, {256, 256, 3.9, 0.64}};
+    // The tile: the one with the least time by a straight line per round of 256 tiles (`chunk` and, of fp32 and of Sign outputs, `round` of each, in us but
+    // for a common factor), fitted to 378 products measured with each of the five (256 to 16384 frames, 128 to 4096 inputs, 1000 to 4096 outputs: the tile
+    // chosen takes 1.1 % more than the best one on average, 12 % at most).  us with tiles of 64 x 64, 128 x 64, 128 x 128, 256 x 128, 256 x 256:
+    // 512 x 2048 x 2048 6.2, 7.1, 8.6, 11.2, 15.7;  2048 x 2048 x 2048 14.0, 12.8, 12.0, 13.7, 17.9;  2048 x 4096 x 3400 38, 34, 26.9, 25.3, 29.8;
+    // 4096 x 2048 x 3400 39, 32, 29.3, 30.1, 26.5;  8192 x 4096 x 3400 140, 111, 87, 91, 73.
+    struct { int rows, cols; double chunk, round[2]; } const kTiles[] = {
+        {64, 64, 0.215, {0.11, 0.18}}, {128, 64, 0.264, {0.29, 0.35}}, {128, 128, 0.37, {1.24, 0.65}}, {256, 128, 0.57, {7.5, 4.0}}, {256, 256, 0.86, {10.4, 3.2}}};
     int tile = 0;
     double least = 0.0;
-    for (int t = 0; t < (K < 768 ? 3 : 5); ++t) {
+    for (int t = 0; t < 5; ++t) {
         const int64_t gx = (M + kTiles[t].rows - 1) / kTiles[t].rows, gy = (N + kTiles[t].cols - 1) / kTiles[t].cols;
         if (gx > 1 << 23 || gy > 65535) continue;   // (2^31 threads along x; 2^30 frames of 128, 2^22 outputs of 128 are inside)
-        const double time = (double)((gx * gy + 255) / 256) * (kTiles[t].round + kTiles[t].chunk * (double)mx4_chunks(K));
+        const double time = (double)((gx * gy + 255) / 256) * (kTiles[t].round[act == BNN_ACT_SIGN] + kTiles[t].chunk * (double)mx4_chunks(K));
         if (least == 0.0 || time < least) tile = t, least = time;
     }
-// From the third round of the largest tile on a workgroup per CU stays for all of its tiles, so that neither the first stages of a tile nor the outputs
+    // From the third round of the largest tile on a workgroup per CU stays for all of its tiles, so that neither the first stages of a tile nor the outputs
     // of the one before stand alone: 16384 x 1024 x 4096 71 -> 67 us (to Sign 49 -> 44), 65536 x 2048 x 2048 185 -> 175, 16384 x 4096 x 4096 156 -> 153, where power
     // is what bounds it.  (In two rounds the CUs with one tile wait for those with two either way: 8192 x 4096 x 3400 73 -> 75.)
     const bool run = tile == 4 && ((M + 255) / 256) * ((N + 255) / 256) > 2 * kMx4Groups && mx4_chunks(K) >= 8;

@@ -183,12 +183,12 @@ def layer(G, bnn, xq, wq, bias, M, K, N, act, wb=32, offset=0):
 LAYERS = [(1, 1, 1), (1, 32, 1), (2, 33, 5), (3, 440, 70), (5, 129, 33), (15, 512, 64), (16, 2048, 100), (17, 130, 257), (31, 96, 31), (33, 1000, 65), (64, 128, 128),
           (65, 256, 129), (100, 3000, 40), (127, 384, 255), (129, 127, 300), (200, 640, 513), (257, 2048, 130), (300, 200, 1003), (520, 1100, 260), (1100, 160, 1100), (3000, 130, 1500), (9000, 128, 1700), (20000, 129, 9), (40, 300, 17000),
           (20000, 64, 1000), (70000, 40, 7), (20, 1100, 130), (50, 2100, 300), (64, 1500, 77),
-          (1100, 1500, 3300), (2300, 900, 3300), (3900, 1025, 3363), (8300, 1030, 4000)]
+          (1100, 1500, 3300), (4000, 2050, 1100), (4000, 4000, 1100), (3900, 1025, 3363), (8300, 2500, 4000), (6100, 2000, 8190)]
 
 
 @pytest.mark.parametrize("M,K,N", LAYERS)
 def test_layer_exact_sums(G, bnn, M, K, N):
-    """Products that are multiples of 1/16 up to 144: with K up to 3000 every partial sum has at most 23 bits."""
+    """Products that are multiples of 1/16 up to 144: with K up to 4000 every partial sum has at most 24 bits."""
     rng = np.random.default_rng(M * 31 + K * 7 + N)
     xq, wq = random_packed(rng, M, K, whole=True), random_packed(rng, N, K, whole=True)
     bias = (rng.integers(-64, 65, N) / 4).astype(np.float32)

@@ -204,10 +204,16 @@ def test_sizes_reach_every_tile(host):  # noqa: F811
     from test_gpu_mx4 import LAYERS
     got = host("""
 result = []
-for M, K, N in %r:
-    bnn.bnn_layer_mx4(A, 1 << 55, 0, M, K, N, bnn.BNN_ACT_LINEAR, 32, 1 << 57)
-    result.append(launches()[0]["kernel"])
+for act in (bnn.BNN_ACT_LINEAR, bnn.BNN_ACT_SIGN):
+    for M, K, N in %r:
+        bnn.bnn_layer_mx4(A, 1 << 55, 0, M, K, N, act, 32, 1 << 57)
+        result.append([act, launches()[0]["kernel"]])
 """ % (LAYERS,))
+    for act in (1, 3):
+        check_tiles([k for a, k in got if a == act])
+
+
+def check_tiles(got):
     gemm = [k.split("mx4_gemm_kernelI")[1] for k in got if "mx4_gemm_kernel" in k]   # ... activation, a workgroup per CU for all its tiles
     assert {k[20:].split("E")[1] for k in gemm} == {"Lb0", "Lb1"}
     tiles = {k[:20] for k in gemm}
